@@ -46,7 +46,7 @@ enum { AMPH_F32 = 0, AMPH_BF16 = 1 };
 enum { AMPH_MAX_TREE = 128, AMPH_MAX_TOPK = 16, AMPH_MAX_HEADS_K = 8 };
 
 /* bits of the device status word (amph_device_status) */
-enum { AMPH_DEV_SAL_OVERFLOW = 1, AMPH_DEV_KV_OVERFLOW = 2, AMPH_DEV_BAD_TOKEN = 4 };
+enum { AMPH_DEV_SAL_OVERFLOW = 1, AMPH_DEV_KV_OVERFLOW = 2, AMPH_DEV_BAD_TOKEN = 4, AMPH_DEV_BAD_PAGE = 8 };
 
 typedef struct amph_config {
   int32_t d_model, n_heads, head_dim; /* d_model = n_heads * head_dim; head_dim is 64 or 128        */
@@ -298,6 +298,79 @@ amph_status amph_pack_kv(amph_ctx *ctx, const void *k_rows, const void *v_rows, 
                          int n_caches);
 amph_status amph_unpack_kv(amph_ctx *ctx, const void *k_tiled, const void *v_tiled, void *k_rows, void *v_rows,
                            int n_caches);
+
+/* ---- a paged key-value cache: plain decoding, one token at a time, and caches held to a budget ------------------
+ * Beside the speculative step: sequences that decode one token each (a batch too large for drafting to pay, or no draft), whose
+ * rows live in pages of a shared pool, and whose caches may be held to a number of rows by eviction.  The calls work on
+ * any number of sequences (not cfg.batch); of the configuration they use n_heads, head_dim, dtype and rope_theta.
+ * Row r of sequence b lies in row r % page_rows of page page_table[b, r / page_rows].  What a page holds of one key head,
+ * page_rows * head_dim elements of K and as many of V, is step-tiled as amph_verify_attn describes.  Elements of key head h of page p
+ * of layer l begin at l * layer_stride + p * page_stride + h * head_stride.  In a pool [n_layers, n_pages, n_kv_heads, page] these are
+ * n_pages * n_kv_heads, n_kv_heads and 1 times page_rows * head_dim.  The caches of amph_target_forward, [n_layers, B, n_heads,
+ * max_kv * head_dim], can be read the same way where max_kv is a multiple of page_rows: layer_stride = B * n_heads * max_kv * head_dim,
+ * page_stride = page_rows * head_dim, head_stride = max_kv * head_dim, and rows [i * page_rows, ...) of sequence b are page
+ * b * n_heads * max_kv / page_rows + i.
+ * Several entries of the table may name the same page (a shared prefix) as long as nothing writes its rows: not amph_paged_append, and
+ * not amph_paged_evict. */
+typedef struct amph_paged_kv {
+  void *k_pages, *v_pages;      /* T, 16-byte aligned                                                              */
+  const int32_t *page_table;    /* [n_seq, table_pages]; entries are looked at only where a sequence has rows       */
+  int32_t n_seq;                /* 1..AMPH_MAX_SEQ                                                                  */
+  int32_t n_kv_heads;           /* divides cfg.n_heads: query head i attends to key head i / (n_heads / n_kv_heads) */
+  int32_t page_rows;            /* multiple of 32                                                                   */
+  int32_t n_pages;              /* entries outside [0, n_pages) are refused (AMPH_DEV_BAD_PAGE)                     */
+  int32_t table_pages;          /* entries of a row of the table; table_pages * page_rows <= 2^24                   */
+  int32_t max_pages;            /* 1..table_pages: no sequence has rows beyond these pages in the calls it is given to.
+                                   A tight bound saves launches and workspace where sequences are short              */
+  int64_t page_stride, head_stride, layer_stride;   /* elements; multiples of 16 bytes                              */
+} amph_paged_kv;
+enum { AMPH_MAX_SEQ = 1024 };
+
+/* Bytes of scratch (16-byte aligned) for the calls below on a cache of this form.  n_layers = 0: amph_paged_attn without
+ * weights; n_layers >= 1: amph_paged_attn with weights, and amph_paged_evict over so many layers. */
+amph_status amph_paged_bytes(amph_ctx *ctx, const amph_paged_kv *kv /* host */, int n_layers, size_t *bytes /* host */);
+
+/* Writes new rows into the pages of one layer.  For every sequence b and j < n_valid[b] (NULL: n_new; clamped to 0..n_new): the key,
+ * rotated at its position (RoPE, base cfg.rope_theta), and the value become row kv_len[b] + j, and the rotated query goes to
+ * q_out.  kv_len is not advanced: every layer of a step is given the same lengths.
+ *   q [n_seq, n_new] rows ld_q elements apart, each [n_heads, head_dim] T; k, v the same with n_kv_heads (the three parts of one
+ *     projection's output, for instance).  Pointers and row distances are multiples of 16 bytes.
+ *   q_out [n_seq, n_new, n_heads, head_dim] T; it may be q itself where ld_q = n_heads * head_dim.  q and q_out may both be NULL.
+ *   pos   [n_seq, n_new] int32: positions, >= 0; NULL: kv_len[b] + j (a cache that has lost rows has other positions than rows)
+ *   weights [n_seq, n_kv_heads, table_pages * page_rows] float32 or NULL: zero for the new rows.
+ *   row_pos [the same] int32 or NULL: the new rows' positions.
+ * Angles are computed in 64 bits.  Device-side errors: kv_len[b] outside [0, max_pages * page_rows] or too few rows left
+ * (AMPH_DEV_KV_OVERFLOW): nothing is written for the sequence.  AMPH_DEV_BAD_PAGE: nothing is written for the new rows in that page. */
+amph_status amph_paged_append(amph_ctx *ctx, const amph_paged_kv *kv /* host */, int layer, int n_new, const int32_t *n_valid,
+                              const int32_t *kv_len, const int32_t *pos, const void *q, int64_t ld_q, const void *k, int64_t ld_k,
+                              const void *v, int64_t ld_v, void *q_out, float *weights, int32_t *row_pos);
+
+/* Attention of one token of every sequence over its rows of one layer, rows = kv_len[b] + n_valid[b] (NULL: n_new; n_new = 0: kv_len[b]):
+ *   out[b, i] = sum_r p_ir v_r,   p_i = softmax over the rows of q[b, i] . k_r / sqrt(head_dim),   r of key head i / (n_heads / n_kv_heads)
+ *   weights_out[b, h, r] = weights_in[b, h, r] + sum of p_ir over the query heads i of key head h
+ * A sequence without rows has out = 0.  Rows behind the last may hold anything.  No order of sums depends on timing.
+ *   q   row b at b * ld_q elements, [n_heads, head_dim] T        out [n_seq, n_heads, head_dim] T, not q itself
+ *   weights_in, weights_out [n_seq, n_kv_heads, table_pages * page_rows] float32: weights_out NULL: none are computed; weights_in NULL:
+ *     zeros; they may be the same.  Places behind the last row are left as they are.
+ * Device-side errors, for which nothing is written for the sequence: AMPH_DEV_KV_OVERFLOW as above, AMPH_DEV_BAD_PAGE. */
+amph_status amph_paged_attn(amph_ctx *ctx, const amph_paged_kv *kv /* host */, int layer, const void *q, int64_t ld_q, int n_new,
+                            const int32_t *n_valid, const int32_t *kv_len, void *out, const float *weights_in, float *weights_out,
+                            void *workspace);
+
+/* Holds every sequence to `budget` rows in all layers, each key head choosing its own.  Of more rows (kv_len[b] + n_valid[b], or n_new) the
+ * call keeps those with row_pos > (the largest row_pos) - recent, then those of the largest weights (NaN last), among equals
+ * the lower row, `budget` in all.  Kept rows below the budget stay where they are; the i-th dropped row below it (ascending)
+ * receives the i-th kept row behind it: key, value, weight and position.  Attention does not depend on the order of rows,
+ * and keys carry their rotation, so nothing else has to move; a step that adds one row moves one at most.
+ *   weights, row_pos [n_layers, n_seq, n_kv_heads, table_pages * page_rows]: _in and _out may be the same; places of _out behind the kept
+ *     rows are left as they are.
+ *   kv_len_out [n_seq]: min(rows, budget); may be kv_len.  This also commits the step's new rows: with budget =
+ *     max_pages * page_rows nothing is dropped.
+ *   1 <= budget; 0 <= recent <= budget
+ * Device-side errors (AMPH_DEV_KV_OVERFLOW, AMPH_DEV_BAD_PAGE in any page that holds rows): the sequence stays as it was, kv_len_out = kv_len. */
+amph_status amph_paged_evict(amph_ctx *ctx, const amph_paged_kv *kv /* host */, int n_layers, int budget, int recent, int n_new,
+                             const int32_t *n_valid, const int32_t *kv_len, int32_t *kv_len_out, const float *weights_in,
+                             float *weights_out, const int32_t *row_pos_in, int32_t *row_pos_out, void *workspace);
 
 /* ---- choice of the verification-attention kernel, for tests and measurements -----------------------
  * The tree attention (amph_verify_attn, and inside amph_target_forward) has two kernels with the same

@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(HERE, "libamph.so")
 
 AMPH_OK, AMPH_EINVAL, AMPH_ESHAPE, AMPH_ETREE, AMPH_EHIP = 0, 1, 2, 3, 4
 AMPH_F32, AMPH_BF16 = 0, 1
-AMPH_DEV_SAL_OVERFLOW, AMPH_DEV_KV_OVERFLOW, AMPH_DEV_BAD_TOKEN = 1, 2, 4
+AMPH_DEV_SAL_OVERFLOW, AMPH_DEV_KV_OVERFLOW, AMPH_DEV_BAD_TOKEN, AMPH_DEV_BAD_PAGE = 1, 2, 4, 8
+AMPH_MAX_SEQ = 1024
 KERNEL_KINDS = ["fc", "sal_qkv", "sal_attn", "sal_wo", "sal_gateup", "sal_down", "head_mlp", "aeb_qkv", "aeb_attn", "aeb_wo",
                 "lm_head", "topk", "t_rmsnorm", "t_qkv", "verify", "t_wo", "t_gateup", "t_down", "t_lmhead"]
 STATUS_NAMES = {0: "AMPH_OK", 1: "AMPH_EINVAL", 2: "AMPH_ESHAPE", 3: "AMPH_ETREE", 4: "AMPH_EHIP"}
@@ -47,6 +48,12 @@ class amph_draft_w(C.Structure):
                 ("aeb2_wv", C.c_void_p), ("aeb2_wo", C.c_void_p), ("lm_a", C.c_void_p), ("lm_b", C.c_void_p)]
 
 
+class amph_paged_kv(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_seq", "n_kv_heads", "page_rows", "n_pages", "table_pages", "max_pages")] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "layer_stride")]
+
+
 EXPORTS = {
     "amph_create": (C.c_int, [C.POINTER(amph_config), C.POINTER(C.c_void_p)]),
     "amph_destroy": (None, [C.c_void_p]),
@@ -71,6 +78,11 @@ EXPORTS = {
                             + [C.c_void_p] * 13),
     "amph_tiled_bytes": (C.c_int, [C.c_void_p, C.c_int, C.POINTER(C.c_size_t)]),
     "amph_pack_weights": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "amph_paged_bytes": (C.c_int, [C.c_void_p, C.POINTER(amph_paged_kv), C.c_int, C.POINTER(C.c_size_t)]),
+    "amph_paged_append": (C.c_int, [C.c_void_p, C.POINTER(amph_paged_kv), C.c_int, C.c_int] + [C.c_void_p] * 3
+                          + [C.c_void_p, C.c_int64] * 3 + [C.c_void_p] * 3),
+    "amph_paged_attn": (C.c_int, [C.c_void_p, C.POINTER(amph_paged_kv), C.c_int, C.c_void_p, C.c_int64, C.c_int] + [C.c_void_p] * 6),
+    "amph_paged_evict": (C.c_int, [C.c_void_p, C.POINTER(amph_paged_kv)] + [C.c_int] * 4 + [C.c_void_p] * 8),
     "amph_verify_kernel": (C.c_int, [C.c_void_p, C.c_int]),
     "amph_profile_kind": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int]),
     "amph_profile_read": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
@@ -292,6 +304,28 @@ class Context:
 
     def amph_pack_weights(self, role: int, w0, w1, w2, dst):
         self._check(lib().amph_pack_weights(self.handle, role, _ptr(w0), _ptr(w1), _ptr(w2), _ptr(dst)), "amph_pack_weights")
+
+    def amph_paged_workspace_bytes(self, kv: amph_paged_kv, n_layers: int = 0) -> int:
+        n = C.c_size_t()
+        self._check(lib().amph_paged_bytes(self.handle, C.byref(kv), n_layers, C.byref(n)), "amph_paged_bytes")
+        return n.value
+
+    def amph_paged_append(self, kv: amph_paged_kv, layer, n_new, n_valid, kv_len, pos, q, ld_q, k, ld_k, v, ld_v, q_out=None,
+                          weights=None, row_pos=None):
+        self._check(lib().amph_paged_append(self.handle, C.byref(kv), layer, n_new, _ptr(n_valid), _ptr(kv_len), _ptr(pos), _ptr(q),
+                                            ld_q, _ptr(k), ld_k, _ptr(v), ld_v, _ptr(q_out), _ptr(weights), _ptr(row_pos)),
+                    "amph_paged_append")
+
+    def amph_paged_attn(self, kv: amph_paged_kv, layer, q, ld_q, n_new, n_valid, kv_len, out, weights_in=None, weights_out=None,
+                        workspace=None):
+        self._check(lib().amph_paged_attn(self.handle, C.byref(kv), layer, _ptr(q), ld_q, n_new, _ptr(n_valid), _ptr(kv_len), _ptr(out),
+                                          _ptr(weights_in), _ptr(weights_out), _ptr(workspace)), "amph_paged_attn")
+
+    def amph_paged_evict(self, kv: amph_paged_kv, n_layers, budget, recent, n_new, n_valid, kv_len, kv_len_out, weights_in, weights_out,
+                         row_pos_in, row_pos_out, workspace):
+        self._check(lib().amph_paged_evict(self.handle, C.byref(kv), n_layers, budget, recent, n_new, _ptr(n_valid), _ptr(kv_len),
+                                           _ptr(kv_len_out), _ptr(weights_in), _ptr(weights_out), _ptr(row_pos_in), _ptr(row_pos_out),
+                                           _ptr(workspace)), "amph_paged_evict")
 
     def amph_verify_kernel(self, kernel: int):
         self._check(lib().amph_verify_kernel(self.handle, kernel), "amph_verify_kernel")

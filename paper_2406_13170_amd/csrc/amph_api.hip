@@ -1,6 +1,7 @@
 // C-ABI layer of libamph: argument checks, the host side of the draft tree, workspace layout, and the
 // launch sequences of amph_draft / amph_target_forward.  All arithmetic lives in the kernels.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <map>
@@ -9,6 +10,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "paged_plan.h"
 
 using namespace amph;
 
@@ -65,6 +67,7 @@ struct amph_ctx {
   int prof_every = 1;                 // one launch in this many is timed
   long long prof_seen = 0;            // launches of prof_kind since it was selected
   int verify_kernel = -1;             // amph_verify_kernel: -1 by shape, 0 registers, 1 LDS ring
+  PagedRope rope;                     // of the paged cache's appends
 };
 
 struct amph_tree {
@@ -389,6 +392,8 @@ amph_status amph_create(const amph_config *cfg, amph_ctx **out) {
   ctx->cfg = c;
   ctx->esz = (c.dtype == AMPH_BF16) ? 2 : 4;
   ctx->ws = make_layout(c);
+  for (int i = 0; i < 64; ++i)
+    ctx->rope.turns[i] = i < c.head_dim / 2 ? std::pow((double)c.rope_theta, -2.0 * i / c.head_dim) / 6.283185307179586476925 : 0.0;
   hipError_t e = scratch_for_current_device(&ctx->device, &ctx->static_scratch);
   if (e == hipSuccess) e = hipMalloc(&ctx->dev_status, 256);
   if (e == hipSuccess) e = hipMemset(ctx->dev_status, 0, 256);
@@ -755,6 +760,153 @@ amph_status amph_pack_kv(amph_ctx *ctx, const void *k_rows, const void *v_rows, 
 
 amph_status amph_unpack_kv(amph_ctx *ctx, const void *k_tiled, const void *v_tiled, void *k_rows, void *v_rows, int n_caches) {
   return kv_layout(ctx, "amph_unpack_kv", k_tiled, v_tiled, k_rows, v_rows, n_caches, false);
+}
+
+}  // extern "C"
+
+// What is wrong with a paged cache for contexts of this configuration, or NULL; *shape: whether it is one of the dimensions.
+namespace amph {
+static_assert(PAGED_MAX_SEQ == AMPH_MAX_SEQ, "the header's limit is the kernels'");
+const char *paged_kv_fault(const amph_config &c, const amph_paged_kv *kv, int n_layers, bool *shape) {
+  const int64_t esz = c.dtype == AMPH_BF16 ? 2 : 4;
+  *shape = false;
+  if (!kv || !kv->k_pages || !kv->v_pages || !kv->page_table) return "null cache, pages or table";
+  if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages) || ((uintptr_t)kv->page_table & 3)) return "misaligned pages or table";
+  if (kv->n_seq < 1 || kv->n_kv_heads < 1 || kv->page_rows < 1 || kv->n_pages < 1 || kv->table_pages < 1 || kv->max_pages < 1 || n_layers < 0)
+    return "sizes must be positive";
+  if (kv->page_stride < 0 || kv->head_stride < 0 || kv->layer_stride < 0 || kv->page_stride * esz % 16 || kv->head_stride * esz % 16 ||
+      kv->layer_stride * esz % 16)
+    return "strides must be multiples of 16 bytes, none negative";
+  *shape = true;
+  if (kv->n_seq > PAGED_MAX_SEQ) return "more than AMPH_MAX_SEQ sequences";
+  if (c.n_heads % kv->n_kv_heads) return "n_kv_heads does not divide n_heads";
+  if (kv->page_rows % 32) return "page_rows must be a multiple of 32";
+  if (kv->max_pages > kv->table_pages) return "max_pages beyond table_pages";
+  if ((int64_t)kv->table_pages * kv->page_rows > (1 << 24)) return "more than 2^24 rows a sequence";
+  constexpr int64_t far = (int64_t)1 << 46;                // elements: offsets in bytes stay below 2^48 each
+  if (kv->page_stride > far / kv->n_pages || kv->head_stride > far / kv->n_kv_heads || kv->layer_stride > far / std::max(n_layers, 1))
+    return "strides too large";
+  if ((int64_t)std::max(n_layers, 1) * kv->n_seq * kv->n_kv_heads > (1 << 30)) return "too many layers";
+  return nullptr;
+}
+}  // namespace amph
+
+namespace {
+
+amph_status check_paged(amph_ctx *ctx, const amph_paged_kv *kv, int n_layers, const char *who) {
+  bool shape = false;
+  if (const char *what = paged_kv_fault(ctx->cfg, kv, n_layers, &shape))
+    return fail(ctx, shape ? AMPH_ESHAPE : AMPH_EINVAL, std::string(who) + ": " + what);
+  return AMPH_OK;
+}
+// also for a call that launches: the tables and pages of another device than the current one are not for its kernels
+amph_status check_paged_call(amph_ctx *ctx, const amph_paged_kv *kv, int n_layers, int n_new, const char *who) {
+  if (amph_status s = check_paged(ctx, kv, n_layers, who)) return s;
+  if (n_new < 0) return fail(ctx, AMPH_EINVAL, std::string(who) + ": negative n_new");
+  if (n_new > kv->max_pages * kv->page_rows) return fail(ctx, AMPH_ESHAPE, std::string(who) + ": n_new beyond max_pages * page_rows");
+  int dev = -1;
+  HIP_TRY(ctx, hipGetDevice(&dev));
+  if (dev != ctx->device) return fail(ctx, AMPH_EINVAL, std::string(who) + ": the current device is not the one the context was created on");
+  return AMPH_OK;
+}
+PagedPages paged_pages(const amph_ctx *ctx, const amph_paged_kv *kv, int layer) {
+  PagedPages c;
+  const size_t off = (size_t)layer * kv->layer_stride * ctx->esz;
+  c.k = (char *)kv->k_pages + off; c.v = (char *)kv->v_pages + off; c.table = kv->page_table;
+  c.n_kv = kv->n_kv_heads; c.page_rows = kv->page_rows; c.n_pages = kv->n_pages; c.table_pages = kv->table_pages;
+  c.page_stride = kv->page_stride; c.head_stride = kv->head_stride; c.layer_stride = kv->layer_stride;
+  return c;
+}
+PagedSeqs paged_seqs(const amph_paged_kv *kv, int n_new, const int32_t *n_valid, const int32_t *kv_len) {
+  return {kv_len, n_valid, kv->n_seq, n_new, kv->max_pages * kv->page_rows};
+}
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+amph_status amph_paged_bytes(amph_ctx *ctx, const amph_paged_kv *kv, int n_layers, size_t *bytes) {
+  if (!ctx) return AMPH_EINVAL;
+  if (!bytes) return fail(ctx, AMPH_EINVAL, "amph_paged_bytes: null argument");
+  if (amph_status s = check_paged(ctx, kv, n_layers, "amph_paged_bytes")) return s;
+  const int cap = kv->max_pages * kv->page_rows;
+  *bytes = paged_attn_ws_bytes(kv->n_seq, ctx->cfg.n_heads, kv->n_kv_heads, ctx->cfg.head_dim, cap, n_layers > 0, nullptr, nullptr);
+  if (n_layers > 0) *bytes = std::max(*bytes, paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, cap, nullptr, nullptr));
+  return AMPH_OK;
+}
+
+amph_status amph_paged_append(amph_ctx *ctx, const amph_paged_kv *kv, int layer, int n_new, const int32_t *n_valid,
+                              const int32_t *kv_len, const int32_t *pos, const void *q, int64_t ld_q, const void *k, int64_t ld_k,
+                              const void *v, int64_t ld_v, void *q_out, float *weights, int32_t *row_pos) {
+  if (!ctx) return AMPH_EINVAL;
+  if (!kv_len || !k || !v || (q == nullptr) != (q_out == nullptr)) return fail(ctx, AMPH_EINVAL, "amph_paged_append: null argument");
+  if (layer < 0) return fail(ctx, AMPH_EINVAL, "amph_paged_append: negative layer");
+  if (amph_status s = check_paged_call(ctx, kv, layer, n_new, "amph_paged_append")) return s;
+  if (n_new < 1) return fail(ctx, AMPH_EINVAL, "amph_paged_append: n_new must be at least 1");
+  const int64_t d_h = ctx->cfg.head_dim, n_h = ctx->cfg.n_heads;
+  for (const void *p : {q, k, v, (const void *)q_out})
+    if (!aligned16(p)) return fail(ctx, AMPH_EINVAL, "amph_paged_append: pointers must be 16-byte aligned");
+  if (!aligned4(n_valid) || !aligned4(kv_len) || !aligned4(pos) || !aligned4(weights) || !aligned4(row_pos))
+    return fail(ctx, AMPH_EINVAL, "amph_paged_append: misaligned pointer");
+  if (ld_k < kv->n_kv_heads * d_h || ld_v < kv->n_kv_heads * d_h || (q && ld_q < n_h * d_h))
+    return fail(ctx, AMPH_ESHAPE, "amph_paged_append: rows closer than a row is long");
+  for (int64_t ld : {q ? ld_q : 0, ld_k, ld_v})
+    if (ld * ctx->esz % 16 || ld > (INT64_MAX >> 33)) return fail(ctx, AMPH_EINVAL, "amph_paged_append: rows must be a multiple of 16 bytes apart");
+  if (q && q == q_out && ld_q != n_h * d_h) return fail(ctx, AMPH_EINVAL, "amph_paged_append: q_out may be q only where its rows are dense");
+  PagedAppendArgs a{};
+  a.c = paged_pages(ctx, kv, layer); a.seqs = paged_seqs(kv, n_new, n_valid, kv_len);
+  a.pos = pos; a.q = q; a.k = k; a.v = v; a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.q_out = q_out;
+  a.n_heads = ctx->cfg.n_heads; a.weights = weights; a.row_pos = row_pos; a.dev_status = ctx->dev_status;
+  if (ctx->cfg.dtype == AMPH_BF16) HIP_TRY(ctx, launch_paged_append<bf16_t>(ctx->stream, a, ctx->rope, ctx->cfg.head_dim));
+  else HIP_TRY(ctx, launch_paged_append<float>(ctx->stream, a, ctx->rope, ctx->cfg.head_dim));
+  return AMPH_OK;
+}
+
+amph_status amph_paged_attn(amph_ctx *ctx, const amph_paged_kv *kv, int layer, const void *q, int64_t ld_q, int n_new,
+                            const int32_t *n_valid, const int32_t *kv_len, void *out, const float *weights_in, float *weights_out,
+                            void *workspace) {
+  if (!ctx) return AMPH_EINVAL;
+  if (!q || !kv_len || !out || !workspace || (weights_in && !weights_out)) return fail(ctx, AMPH_EINVAL, "amph_paged_attn: null argument");
+  if (layer < 0) return fail(ctx, AMPH_EINVAL, "amph_paged_attn: negative layer");
+  if (amph_status s = check_paged_call(ctx, kv, layer, n_new, "amph_paged_attn")) return s;
+  const amph_config &c = ctx->cfg;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || ld_q * ctx->esz % 16 || ld_q < 0 || ld_q > (INT64_MAX >> 33))
+    return fail(ctx, AMPH_EINVAL, "amph_paged_attn: q, its rows, out and workspace must be 16-byte aligned");
+  if (!aligned4(n_valid) || !aligned4(kv_len) || !aligned4(weights_in) || !aligned4(weights_out))
+    return fail(ctx, AMPH_EINVAL, "amph_paged_attn: misaligned pointer");
+  if (q == out) return fail(ctx, AMPH_EINVAL, "amph_paged_attn: out must not alias q");
+  PagedAttnArgs a{};
+  a.c = paged_pages(ctx, kv, layer); a.seqs = paged_seqs(kv, n_new, n_valid, kv_len);
+  a.q = q; a.ld_q = ld_q; a.out = out; a.n_heads = c.n_heads; a.weights_in = weights_in; a.weights_out = weights_out;
+  a.dev_status = ctx->dev_status;
+  paged_attn_ws_bytes(kv->n_seq, c.n_heads, kv->n_kv_heads, c.head_dim, a.seqs.cap, weights_out != nullptr, &a, (unsigned char *)workspace);
+  if (c.dtype == AMPH_BF16) HIP_TRY(ctx, launch_paged_attn<bf16_t>(ctx->stream, a, c.head_dim));
+  else HIP_TRY(ctx, launch_paged_attn<float>(ctx->stream, a, c.head_dim));
+  return AMPH_OK;
+}
+
+amph_status amph_paged_evict(amph_ctx *ctx, const amph_paged_kv *kv, int n_layers, int budget, int recent, int n_new,
+                             const int32_t *n_valid, const int32_t *kv_len, int32_t *kv_len_out, const float *weights_in,
+                             float *weights_out, const int32_t *row_pos_in, int32_t *row_pos_out, void *workspace) {
+  if (!ctx) return AMPH_EINVAL;
+  if (!kv_len || !kv_len_out || !weights_in || !weights_out || !row_pos_in || !row_pos_out || !workspace)
+    return fail(ctx, AMPH_EINVAL, "amph_paged_evict: null argument");
+  if (n_layers < 1 || budget < 1 || recent < 0 || recent > budget)
+    return fail(ctx, AMPH_EINVAL, "amph_paged_evict: need n_layers >= 1, budget >= 1 and 0 <= recent <= budget");
+  if (amph_status s = check_paged_call(ctx, kv, n_layers, n_new, "amph_paged_evict")) return s;
+  if (!aligned16(workspace)) return fail(ctx, AMPH_EINVAL, "amph_paged_evict: workspace must be 16-byte aligned");
+  for (const void *p : {(const void *)n_valid, (const void *)kv_len, (const void *)kv_len_out, (const void *)weights_in, (const void *)weights_out,
+                        (const void *)row_pos_in, (const void *)row_pos_out})
+    if (!aligned4(p)) return fail(ctx, AMPH_EINVAL, "amph_paged_evict: misaligned pointer");
+  PagedEvictArgs a{};
+  a.c = paged_pages(ctx, kv, 0); a.seqs = paged_seqs(kv, n_new, n_valid, kv_len);
+  a.budget = budget; a.recent = recent; a.weights_in = weights_in; a.weights_out = weights_out; a.pos_in = row_pos_in;
+  a.pos_out = row_pos_out; a.kv_len_out = kv_len_out; a.dev_status = ctx->dev_status;
+  paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, a.seqs.cap, &a, (unsigned char *)workspace);
+  if (ctx->cfg.dtype == AMPH_BF16) HIP_TRY(ctx, launch_paged_evict<bf16_t>(ctx->stream, a, n_layers, ctx->cfg.head_dim));
+  else HIP_TRY(ctx, launch_paged_evict<float>(ctx->stream, a, n_layers, ctx->cfg.head_dim));
+  return AMPH_OK;
 }
 
 amph_status amph_verify_kernel(amph_ctx *ctx, int kernel) {

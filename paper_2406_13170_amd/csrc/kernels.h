@@ -185,4 +185,46 @@ size_t verify_ws_floats(int B, int T, int n_heads, int d_h, int max_kv, int elem
 size_t verify_partials_floats(int B, int T, int n_heads, int d_h, int max_kv, int elem_bytes, int kernel);
 template <typename T> hipError_t launch_verify_attn(hipStream_t st, const VerifyArgs &a);
 
+// ---- paged.hip (paged key-value cache) ----
+struct PagedPages {           // one layer's pages as the device sees them (amph_paged_kv)
+  void *k, *v;
+  const int32_t *table;
+  int n_kv, page_rows, n_pages, table_pages;
+  size_t page_stride, head_stride, layer_stride;
+};
+struct PagedSeqs {            // rows of sequence b: kv_len[b], then n_valid[b] (NULL: n_new) new ones; at most cap in all
+  const int32_t *kv_len, *n_valid;
+  int n_seq, n_new, cap;
+};
+struct PagedAttnArgs {
+  PagedPages c; PagedSeqs seqs;
+  const void *q; size_t ld_q; void *out;
+  int n_heads;
+  const float *weights_in; float *weights_out;
+  uint32_t *dev_status;
+  int32_t *plan; float2 *stats; float *partials, *scores;        // in the workspace: paged_attn_ws_bytes
+};
+size_t paged_attn_ws_bytes(int n_seq, int n_heads, int n_kv, int d_h, int cap, bool weights, PagedAttnArgs *a, unsigned char *ws);
+template <typename T> hipError_t launch_paged_attn(hipStream_t st, const PagedAttnArgs &a, int d_h);
+struct PagedRope { double turns[64]; };       // theta^(-2 i / d_h) / (2 pi), i < d_h / 2: what a position adds to pair i's angle
+struct PagedAppendArgs {
+  PagedPages c; PagedSeqs seqs;
+  const int32_t *pos;
+  const void *q, *k, *v; size_t ld_q, ld_k, ld_v; void *q_out;
+  int n_heads;
+  float *weights; int32_t *row_pos;
+  uint32_t *dev_status;
+};
+template <typename T> hipError_t launch_paged_append(hipStream_t st, const PagedAppendArgs &a, const PagedRope &rope, int d_h);
+struct PagedEvictArgs {
+  PagedPages c; PagedSeqs seqs;
+  int budget, recent;
+  const float *weights_in; float *weights_out;
+  const int32_t *pos_in; int32_t *pos_out, *kv_len_out;
+  uint32_t *dev_status;
+  int32_t *new_len, *n_moves, *lists;                             // in the workspace: paged_evict_ws_bytes
+};
+size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, PagedEvictArgs *a, unsigned char *ws);
+template <typename T> hipError_t launch_paged_evict(hipStream_t st, const PagedEvictArgs &a, int n_layers, int d_h);
+
 }  // namespace amph

@@ -1,0 +1,798 @@
+// The paged key-value cache: rows written into pages (RoPE on the way), one token's attention over them, and eviction by the
+// attention's accumulated weights.  A page holds page_rows rows of every key head, K and V step-tiled (formulas: header of the
+// C ABI), so a 64-byte column of 16 keys, or 16 dims of a step's values, is again a contiguous 1 KB matrix-core fragment.
+#include <algorithm>
+
+#include "kernels.h"
+#include "paged_plan.h"
+
+namespace amph {
+
+__device__ __forceinline__ float paged_exp2(float x) { return __builtin_amdgcn_exp2f(x); }   // arguments <= 0: no rescue of tiny results
+constexpr int BUF_RAW = 0x00020000;                    // word 3 of a buffer descriptor: plain bytes
+__device__ __forceinline__ uint4 ldb16_stream(__amdgpu_buffer_rsrc_t r, int at) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 2);            // (2: non-temporal)
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+constexpr float PAGED_LOWEST = -3.402823466e38f;       // of a running maximum: no finite score is below it, and -inf - it is -inf
+
+__device__ __forceinline__ int paged_len(const PagedSeqs &s, int b) {
+  return paged_rows(s.kv_len[b], s.n_valid ? paged_new(s.n_new, s.n_valid[b]) : s.n_new, s.cap);
+}
+
+// =====================================================================================================
+// amph_paged_attn
+//   S^T[key, q] = K[key, :] . Q[q, :],   O^T[d, q] += V^T[d, keys] . P^T[keys, q]
+// on the matrix cores as in the verification attention (the accumulator of a score tile is the second product's operand), with
+// the G query heads of a key head as the columns.  Bound by the cache's bytes: every row is read once, for all its query heads.
+// =====================================================================================================
+template <typename T, int DH, int NQB>
+struct PA {
+  static constexpr int PER = Elem<T>::PER;
+  static constexpr int KSTEP = 4 * PER;            // keys per step
+  static constexpr int NT = KSTEP / 16;            // S^T tiles per step
+  static constexpr int DSTEPS = DH / (4 * PER);    // 64-byte pieces of a K/Q row
+  static constexpr int DB = DH / 16;               // 16-row blocks of O^T
+  static constexpr int NQ = NQB * 16;              // queries per workgroup
+  static constexpr int OPITCH = DH + 4;            // floats
+  static constexpr int PART = NQ * DH + 2 * NQ;    // floats of one partial: O, then m, then l (-1: a bad page)
+};
+
+// ALONE: a workgroup for every walk (one key head's query group of one sequence).  Otherwise the walks' key steps are dealt out
+// in equal pieces (paged_plan.h) and k_paged_fold joins what was cut.
+template <typename T, int DH, int NQB, bool ALONE>
+__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
+  using C = PA<T, DH, NQB>;
+  constexpr int PER = C::PER, KSTEP = C::KSTEP, NT = C::NT, DSTEPS = C::DSTEPS, DB = C::DB, NQ = C::NQ;
+  __shared__ __align__(16) float sm_o[PAGED_WAVES][NQ][C::OPITCH];
+  __shared__ float sm_m[PAGED_WAVES][NQ], sm_l[PAGED_WAVES][NQ];
+  __shared__ int sm_len[ALONE ? 1 : PAGED_MAX_SEQ], sm_sum[PAGED_WAVES], sm_at[2];
+
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r16 = lane & 15;
+  const int n_seq = a.seqs.n_seq, G = a.n_heads / a.c.n_kv, n_qg = (G + NQ - 1) / NQ, U = a.c.n_kv * n_qg;
+  const int psteps = a.c.page_rows / KSTEP;            // key steps of a page
+  const float scale = 1.4426950408889634f * rsqrtf((float)DH);
+  const float NEG_INF = -__builtin_huge_valf();
+
+  // ---- the key steps [s, s + n) of one walk
+  auto walk = [&](int b, int u, int L, int s, int n, bool whole, int place) {
+    const int h = u / n_qg, q_base = (u % n_qg) * NQ, live_q = min(G - q_base, NQ);
+    const T *qb0 = (const T *)a.q + (size_t)b * a.ld_q + ((size_t)h * G + q_base) * DH;
+    uint4 Qf[NQB][DSTEPS];                             // queries as B fragments: lane = query r16 of block qb
+    #pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      const int qi = qb * 16 + r16;
+      #pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds)              // padding queries repeat query 0; nothing of theirs is stored
+        Qf[qb][ds] = ldg16(qb0 + (size_t)(qi < live_q ? qi : 0) * DH + ds * (4 * PER) + g * PER);
+    }
+    unsigned char *Kh = (unsigned char *)a.c.k + (size_t)h * a.c.head_stride * sizeof(T);
+    unsigned char *Vh = (unsigned char *)a.c.v + (size_t)h * a.c.head_stride * sizeof(T);
+    const int lane_at = r16 * 64 + g * 16;
+    const int32_t *row_table = a.c.table + (size_t)b * a.c.table_pages;
+    float *score = a.scores ? a.scores + ((size_t)b * a.n_heads + (size_t)h * G + q_base) * a.seqs.cap : nullptr;
+
+    f32x4 O[NQB][DB];
+    float m_run[NQB], l_run[NQB];
+    #pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      m_run[qb] = PAGED_LOWEST; l_run[qb] = 0.f;
+      #pragma unroll
+      for (int db = 0; db < DB; ++db) O[qb][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    bool bad = false;
+
+    // this wave's steps are s + wave + 4 i, i < n_w; lane l keeps where step 64 * block + l begins (bytes into the pages)
+    const int n_w = (n - wave + PAGED_WAVES - 1) / PAGED_WAVES;
+    unsigned long long where = 0;
+    auto look_up = [&](int i0) {
+      const int st = s + wave + PAGED_WAVES * min(i0 + lane, n_w - 1), pg = st / psteps;
+      int id = row_table[pg];
+      if ((unsigned)id >= (unsigned)a.c.n_pages) { bad = true; id = 0; }
+      where = ((unsigned long long)id * a.c.page_stride + (unsigned long long)(st - pg * psteps) * (KSTEP * DH)) * sizeof(T);
+    };
+    auto step_base = [&](int i) -> size_t {            // (uniform)
+      const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)where, i & 63);
+      const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(where >> 32), i & 63);
+      return ((size_t)hi << 32) | lo;
+    };
+    uint4 Kf[NT][DSTEPS], Vf[DB];
+    // A step's fragments through a buffer of its bytes; of no bytes where there is no further step: such loads fetch nothing, and the
+    // loop needs no branch around them.
+    auto load_k = [&](size_t at, bool live) {
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(Kh + at, 0, live ? NT * DSTEPS * 1024 : 0, BUF_RAW);
+      #pragma unroll
+      for (int t = 0; t < NT; ++t)
+        #pragma unroll
+        for (int ds = 0; ds < DSTEPS; ++ds) Kf[t][ds] = ldb16_stream(r, lane_at + (t * DSTEPS + ds) * 1024);
+    };
+    auto load_v = [&](size_t at, bool live) {
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(Vh + at, 0, live ? DB * 1024 : 0, BUF_RAW);
+      #pragma unroll
+      for (int db = 0; db < DB; ++db) Vf[db] = ldb16_stream(r, lane_at + db * 1024);
+    };
+    // scores of step i: keys key0 + g * PER + j, query r16 of every block
+    auto scores = [&](int i, float (&sv)[NQB][PER]) {
+      #pragma unroll
+      for (int qb = 0; qb < NQB; ++qb)
+        #pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+          #pragma unroll
+          for (int ds = 0; ds < DSTEPS; ++ds) acc = mma16<T>(Kf[t][ds], Qf[qb][ds], acc);
+          #pragma unroll
+          for (int c = 0; c < 4; ++c) sv[qb][t * 4 + c] = acc[c] * scale;
+        }
+    };
+    // the running maximum, and the step's probabilities in the place of its scores
+    auto softmax = [&](int i, float (&sv)[NQB][PER]) {
+      const int key0 = (s + wave + PAGED_WAVES * i) * KSTEP;
+      #pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) {
+        if (key0 + KSTEP > L) {
+          #pragma unroll
+          for (int j = 0; j < PER; ++j) if (key0 + g * PER + j >= L) sv[qb][j] = NEG_INF;
+        }
+        if (score && qb * 16 + r16 < live_q) {         // (cap is a multiple of the step: rows behind the last have their place)
+          float *to = score + (size_t)(qb * 16 + r16) * a.seqs.cap + key0 + g * PER;
+          #pragma unroll
+          for (int j = 0; j < PER; j += 4)
+            *reinterpret_cast<float4 *>(to + j) = make_float4(sv[qb][j], sv[qb][j + 1], sv[qb][j + 2], sv[qb][j + 3]);
+        }
+        float mx = sv[qb][0], ls = 0.f;
+        #pragma unroll
+        for (int j = 1; j < PER; ++j) mx = fmaxf(mx, sv[qb][j]);
+        const float mn = fmaxf(m_run[qb], lanes_xor32(lanes_xor16(mx, MaxF()), MaxF()));
+        if (__any(mn > m_run[qb])) {                   // the running maximum rarely moves after the first steps
+          const float corr = paged_exp2(m_run[qb] - mn);
+          l_run[qb] *= corr;
+          #pragma unroll
+          for (int db = 0; db < DB; ++db) O[qb][db] *= corr;
+          m_run[qb] = mn;
+        }
+        #pragma unroll
+        for (int j = 0; j < PER; ++j) { sv[qb][j] = paged_exp2(sv[qb][j] - mn); ls += sv[qb][j]; }
+        l_run[qb] += ls;
+      }
+    };
+    auto values = [&](int i, const float (&pv)[NQB][PER]) {
+      const int key0 = (s + wave + PAGED_WAVES * i) * KSTEP;
+      if (key0 + KSTEP > L) {                          // rows behind the last may hold anything, NaN too: 0 * V has to be 0
+        const int in = L - key0 - g * PER;             // elements of the lane's pieces that are rows
+        unsigned keep[4];
+        #pragma unroll
+        for (int w = 0; w < 4; ++w)
+          keep[w] = sizeof(T) == 4 ? (in > w ? ~0u : 0u) : (in > 2 * w ? 0xffffu : 0u) | (in > 2 * w + 1 ? 0xffff0000u : 0u);
+        #pragma unroll
+        for (int db = 0; db < DB; ++db) { Vf[db].x &= keep[0]; Vf[db].y &= keep[1]; Vf[db].z &= keep[2]; Vf[db].w &= keep[3]; }
+      }
+      #pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) {
+        const uint4 Pf = pack16<T>(pv[qb]);
+        #pragma unroll
+        for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Pf, O[qb][db]);
+        if constexpr (sizeof(T) == 2) {                // what the rounding to bf16 took away, as a second operand: P has 16 bits
+          float hi[PER], rest[PER];
+          Elem<T>::unpack(Pf, hi);
+          #pragma unroll
+          for (int j = 0; j < PER; ++j) rest[j] = pv[qb][j] - hi[j];
+          const uint4 Rf = pack16<T>(rest);
+          #pragma unroll
+          for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Rf, O[qb][db]);
+        }
+      }
+    };
+
+    if (n_w > 0) {
+      // One register set: a step's keys are asked for when the scores of the step before are done, its values when the products
+      // before are.  The other waves of the SIMD cover what is left of the latency.
+      look_up(0);
+      size_t at = step_base(0);
+      load_k(at, true);
+      load_v(at, true);
+      #pragma unroll 1
+      for (int i = 0; i < n_w; ++i) {
+        const bool more = i + 1 < n_w;
+        if (more && ((i + 1) & 63) == 0) look_up(i + 1);
+        at = step_base(i + 1);
+        float sv[NQB][PER];
+        scores(i, sv);
+        load_k(at, more);
+        softmax(i, sv);
+        values(i, sv);
+        load_v(at, more);
+      }
+    }
+    const bool wave_bad = __any(bad);
+
+    // ---- lane groups hold partial sums of l for the same query; then waves -> workgroup through LDS
+    __syncthreads();                                   // the walk before has read its sums
+    #pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      const float l = lanes_xor32(lanes_xor16(l_run[qb], AddF()), AddF());
+      if (g == 0) { sm_m[wave][qb * 16 + r16] = m_run[qb]; sm_l[wave][qb * 16 + r16] = wave_bad ? -1.f : l; }
+      #pragma unroll
+      for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sm_o[wave][qb * 16 + r16][db * 16 + g * 4]) = O[qb][db];
+    }
+    __syncthreads();
+    const bool any_bad = sm_l[0][0] < 0.f || sm_l[1][0] < 0.f || sm_l[2][0] < 0.f || sm_l[3][0] < 0.f;
+    if (any_bad && tid == 0) atomicOr(a.dev_status, (unsigned)AMPH_DEV_BAD_PAGE);
+    float *part = whole ? nullptr : a.partials + (size_t)place * C::PART;
+    for (int idx = tid; idx < live_q * (DH / 4); idx += 256) {        // 4 dims of one query
+      const int q = idx / (DH / 4), d4 = (idx % (DH / 4)) * 4;
+      float mw = sm_m[0][q], l = 0.f;
+      #pragma unroll
+      for (int w = 1; w < PAGED_WAVES; ++w) mw = fmaxf(mw, sm_m[w][q]);
+      f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+      #pragma unroll
+      for (int w = 0; w < PAGED_WAVES; ++w) {
+        const float f = paged_exp2(sm_m[w][q] - mw);
+        o += *reinterpret_cast<const f32x4 *>(&sm_o[w][q][d4]) * f;
+        l += sm_l[w][q] * f;
+      }
+      if (any_bad) l = -1.f;
+      const size_t head = (size_t)b * a.n_heads + (size_t)h * G + q_base + q;
+      if (whole) {
+        const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+        const float r[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        if (!any_bad) store4<T>((T *)a.out + head * DH + d4, r);
+        if (score && d4 == 0) a.stats[head] = make_float2(mw, l);
+      } else {
+        *reinterpret_cast<f32x4 *>(part + (size_t)q * DH + d4) = o;
+        if (d4 == 0) { part[NQ * DH + q] = mw; part[NQ * DH + NQ + q] = l; }
+      }
+    }
+  };
+
+  if constexpr (ALONE) {
+    const int b = blockIdx.x / U, u = blockIdx.x % U, L = paged_len(a.seqs, b);
+    if (L < 0) {                                       // (whole workgroup)
+      if (tid == 0 && u == 0) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
+      return;
+    }
+    walk(b, u, L, 0, (L + KSTEP - 1) / KSTEP, true, 0);
+    return;
+  }
+
+  // ---- the sequences' lengths and the steps before each, thread t for sequences 4 t .. 4 t + 3
+  constexpr int PT = PAGED_MAX_SEQ / 256;
+  int st[PT], sum = 0;
+  bool over = false;
+  #pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    const int b = tid * PT + i;
+    int L = 0;
+    if (b < n_seq) {
+      L = paged_len(a.seqs, b);
+      sm_len[b] = L;
+      over |= L < 0;
+    }
+    st[i] = L > 0 ? (L + KSTEP - 1) / KSTEP : 0;
+    sum += st[i];
+  }
+  int upto = sum;
+  #pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) {
+    const int v = __shfl_up(upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == WAVE - 1) sm_sum[wave] = upto;
+  if (blockIdx.x == 0 && over) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
+  __syncthreads();
+  int before = upto - sum, all = 0;
+  #pragma unroll
+  for (int w = 0; w < PAGED_WAVES; ++w) { before += w < wave ? sm_sum[w] : 0; all += sm_sum[w]; }
+  const long long total = (long long)all * U;
+  const int chunk = paged_chunk(total, gridDim.x);
+  const long long first = (long long)blockIdx.x * chunk;
+  #pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    const int b = tid * PT + i;
+    if (b < n_seq) {
+      if (blockIdx.x == 0) { a.plan[b] = before; a.plan[n_seq + 1 + b] = sm_len[b]; }
+      const long long off = first - (long long)before * U;
+      if (off >= 0 && off < (long long)st[i] * U) { sm_at[0] = b; sm_at[1] = (int)off; }
+    }
+    before += st[i];
+  }
+  if (blockIdx.x == 0 && tid == 0) a.plan[n_seq] = all;
+  if (first >= total) return;                          // (whole workgroup)
+  __syncthreads();
+  int b = sm_at[0], u, s, left = (int)min((long long)chunk, total - first);
+  bool head_of_piece = true;
+  {
+    const int steps = (sm_len[b] + KSTEP - 1) / KSTEP;
+    u = sm_at[1] / steps;
+    s = sm_at[1] - u * steps;
+  }
+  while (left > 0) {
+    const int L = sm_len[b], steps = (L + KSTEP - 1) / KSTEP, n = min(steps - s, left);
+    walk(b, u, L, s, n, n == steps, 2 * blockIdx.x + (head_of_piece ? 0 : 1));
+    head_of_piece = false;
+    left -= n;
+    s = 0;
+    if (++u == U) {
+      u = 0;
+      do ++b; while (left > 0 && sm_len[b] <= 0);      // (steps are left: so is a sequence that has them)
+    }
+  }
+}
+
+// Joins the walks that were cut: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m) over a walk's pieces; writes zeros for a
+// sequence without rows; and, where weights are asked for, adds every row's probabilities up from the scores that the walks left.
+// Workgroups [0, n_seq * n_heads): a query's output each; those behind: 1024 rows of one key head each.
+constexpr int PAGED_WROWS = 1024;
+
+template <typename T, int DH, int NQB>
+__global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, int wgs, int row_wgs) {
+  using C = PA<T, DH, NQB>;
+  constexpr int KSTEP = C::KSTEP, NQ = C::NQ, LPQ = DH / 4, NG = 256 / LPQ;
+  __shared__ __align__(16) float sm_o[NG][DH];
+  __shared__ float sm_m[NG], sm_l[NG];
+  __shared__ float2 sm_ml[32];
+  const int tid = threadIdx.x, n_seq = a.seqs.n_seq, G = a.n_heads / a.c.n_kv, n_qg = (G + NQ - 1) / NQ, U = a.c.n_kv * n_qg;
+  const bool alone = wgs == 0;
+  const int outs = alone ? 0 : n_seq * a.n_heads;
+  const int item = (int)blockIdx.x - outs;
+  const int bh = item < 0 ? blockIdx.x : item / row_wgs;                       // (sequence, head) or (sequence, key head)
+  const int b = item < 0 ? bh / a.n_heads : bh / a.c.n_kv;
+  const int L = alone ? paged_len(a.seqs, b) : a.plan[n_seq + 1 + b];
+  if (L < 0) return;
+  const int steps = (L + KSTEP - 1) / KSTEP;
+  const int pre = alone ? 0 : a.plan[b];
+  const int chunk = alone ? 1 : paged_chunk((long long)a.plan[n_seq] * U, wgs);
+
+  if (item < 0) {
+    const int head = bh % a.n_heads, h = head / G, q = head % G, d4 = (tid % LPQ) * 4, grp = tid / LPQ;
+    T *dst = (T *)a.out + (size_t)bh * DH + d4;
+    if (L == 0) {
+      const float z[4] = {0.f, 0.f, 0.f, 0.f};
+      if (grp == 0) store4<T>(dst, z);
+      return;
+    }
+    const PagedWalk wk = paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, chunk);
+    if (wk.w0 == wk.w1) return;                        // one workgroup had the whole walk and wrote its output
+    const int np = wk.w1 - wk.w0 + 1, qi = q % NQ;
+    // the chain of round trips is what this costs: four pieces a thread are asked for at once
+    constexpr int FU = 4;
+    float m = PAGED_LOWEST, l = 0.f;
+    f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+    bool bad = false;
+    for (int i0 = grp; i0 < np; i0 += NG * FU) {
+      float ms[FU], ls[FU];
+      f32x4 os[FU];
+      #pragma unroll
+      for (int k = 0; k < FU; ++k) {
+        const float *p = a.partials + (size_t)wk.place(wk.w0 + min(i0 + k * NG, np - 1)) * C::PART;
+        ms[k] = p[NQ * DH + qi];
+        ls[k] = p[NQ * DH + NQ + qi];
+        os[k] = *reinterpret_cast<const f32x4 *>(p + (size_t)qi * DH + d4);
+      }
+      #pragma unroll
+      for (int k = 0; k < FU; ++k) {
+        if (i0 + k * NG >= np) continue;
+        bad |= ls[k] < 0.f;
+        const float mn = fmaxf(m, ms[k]), f0 = paged_exp2(m - mn), f1 = paged_exp2(ms[k] - mn);
+        o = o * f0 + os[k] * f1;
+        l = l * f0 + ls[k] * f1;
+        m = mn;
+      }
+    }
+    *reinterpret_cast<f32x4 *>(&sm_o[grp][d4]) = o;
+    if (d4 == 0) { sm_m[grp] = m; sm_l[grp] = l; }
+    if (__syncthreads_or(bad)) return;
+    if (grp != 0) return;
+    float mt = PAGED_LOWEST, lt = 0.f;
+    f32x4 ot = (f32x4){0.f, 0.f, 0.f, 0.f};
+    #pragma unroll
+    for (int k = 0; k < NG; ++k) mt = fmaxf(mt, sm_m[k]);
+    #pragma unroll
+    for (int k = 0; k < NG; ++k) {
+      const float f = paged_exp2(sm_m[k] - mt);
+      ot += *reinterpret_cast<const f32x4 *>(&sm_o[k][d4]) * f;
+      lt += sm_l[k] * f;
+    }
+    const float inv = lt > 0.f || lt != lt ? 1.0f / lt : 0.f;
+    const float r[4] = {ot[0] * inv, ot[1] * inv, ot[2] * inv, ot[3] * inv};
+    store4<T>(dst, r);
+    return;
+  }
+
+  // ---- weights of rows [row0, row0 + 1024) of key head h: thread t has four of them
+  const int h = bh % a.c.n_kv, row0 = (item % row_wgs) * PAGED_WROWS, row = row0 + tid * 4;
+  if (row0 >= L) return;
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  bool bad = false;
+  for (int qa = 0; qa < G; qa += 32) {                 // 32 queries' maxima and sums at a time, eight lanes for each
+    const int q = qa + tid / 8, t8 = tid & 7;
+    float m = PAGED_LOWEST, l = 0.f;
+    if (q < G) {
+      const PagedWalk wk = alone ? PagedWalk{0, 0, true}
+                                 : paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, chunk);
+      if (wk.w0 == wk.w1) {
+        const float2 st = a.stats[(size_t)b * a.n_heads + h * G + q];
+        if (t8 == 0) { m = st.x; l = st.y; bad |= l < 0.f; }
+      } else {
+        for (int i = t8; i <= wk.w1 - wk.w0; i += 8) {
+          const float *p = a.partials + (size_t)wk.place(wk.w0 + i) * C::PART + NQ * DH + q % NQ;
+          const float mi = p[0], li = p[NQ], mn = fmaxf(m, mi);
+          bad |= li < 0.f;
+          l = l * paged_exp2(m - mn) + li * paged_exp2(mi - mn);
+          m = mn;
+        }
+      }
+    }
+    #pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      const float mo = __shfl_xor(m, o), lo = __shfl_xor(l, o), mn = fmaxf(m, mo);
+      l = l * paged_exp2(m - mn) + lo * paged_exp2(mo - mn);
+      m = mn;
+    }
+    __syncthreads();
+    if (t8 == 0) sm_ml[tid / 8] = make_float2(m, l > 0.f || l != l ? 1.0f / l : 0.f);
+    if (__syncthreads_or(bad)) return;
+    if (row < L) {
+      const float *sc = a.scores + ((size_t)b * a.n_heads + (size_t)h * G + qa) * a.seqs.cap + row;
+      for (int i = 0; i < min(32, G - qa); ++i) {
+        const float4 v = *reinterpret_cast<const float4 *>(sc + (size_t)i * a.seqs.cap);
+        const float2 ml = sm_ml[i];
+        acc[0] += paged_exp2(v.x - ml.x) * ml.y; acc[1] += paged_exp2(v.y - ml.x) * ml.y;
+        acc[2] += paged_exp2(v.z - ml.x) * ml.y; acc[3] += paged_exp2(v.w - ml.x) * ml.y;
+      }
+    }
+  }
+  const size_t at = (size_t)bh * a.c.table_pages * a.c.page_rows + row;
+  #pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (row + i < L) a.weights_out[at + i] = (a.weights_in ? a.weights_in[at + i] : 0.f) + acc[i];
+}
+
+int paged_query_blocks(int group) { return group > 16 ? 2 : 1; }
+
+// Up to this many key steps a wave walks by itself costs less than the launch of a fold.
+static bool paged_alone(const PagedAttnArgs &a, int kstep) { return a.seqs.cap <= 4 * PAGED_WAVES * kstep; }
+
+size_t paged_attn_ws_bytes(int n_seq, int n_heads, int n_kv, int d_h, int cap, bool weights, PagedAttnArgs *a, unsigned char *ws) {
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t o = at; at = (at + n + 255) / 256 * 256; return ws ? ws + o : nullptr; };
+  const int nq = 16 * paged_query_blocks(n_heads / n_kv);
+  unsigned char *plan = take((size_t)(2 * n_seq + 1) * 4), *stats = take((size_t)n_seq * n_heads * 8);
+  unsigned char *part = take((size_t)2 * PAGED_WGS * (nq * d_h + 2 * nq) * 4);
+  unsigned char *scores = weights ? take((size_t)n_seq * n_heads * cap * 4) : nullptr;
+  if (a) { a->plan = (int32_t *)plan; a->stats = (float2 *)stats; a->partials = (float *)part; a->scores = (float *)scores; }
+  return at;
+}
+
+template <typename T, int DH, int NQB>
+static hipError_t paged_attn_shape(hipStream_t st, const PagedAttnArgs &a) {
+  using C = PA<T, DH, NQB>;
+  const int G = a.n_heads / a.c.n_kv, walks = a.seqs.n_seq * a.c.n_kv * ((G + C::NQ - 1) / C::NQ);
+  const bool alone = paged_alone(a, C::KSTEP), weights = a.weights_out != nullptr;
+  if (alone)
+    hipLaunchKernelGGL((k_paged_attn<T, DH, NQB, true>), dim3(walks), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_paged_attn<T, DH, NQB, false>), dim3(PAGED_WGS), dim3(256), 0, st, a);
+  const int row_wgs = weights ? (a.seqs.cap + PAGED_WROWS - 1) / PAGED_WROWS : 0;
+  const long long grid = (alone ? 0ll : (long long)a.seqs.n_seq * a.n_heads) + (long long)a.seqs.n_seq * a.c.n_kv * row_wgs;
+  if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+  if (grid)
+    hipLaunchKernelGGL((k_paged_fold<T, DH, NQB>), dim3((unsigned)grid), dim3(256), 0, st, a, alone ? 0 : PAGED_WGS, std::max(row_wgs, 1));
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_paged_attn(hipStream_t st, const PagedAttnArgs &a, int d_h) {
+  const int nqb = paged_query_blocks(a.n_heads / a.c.n_kv);
+  if (d_h == 128) return nqb == 2 ? paged_attn_shape<T, 128, 2>(st, a) : paged_attn_shape<T, 128, 1>(st, a);
+  return nqb == 2 ? paged_attn_shape<T, 64, 2>(st, a) : paged_attn_shape<T, 64, 1>(st, a);
+}
+template hipError_t launch_paged_attn<float>(hipStream_t, const PagedAttnArgs &, int);
+template hipError_t launch_paged_attn<bf16_t>(hipStream_t, const PagedAttnArgs &, int);
+
+// =====================================================================================================
+// amph_paged_append
+// A workgroup has one key step's rows of one sequence (those of them that are new) for some of the heads: first the rows' cosines
+// and sines into LDS, then a wave takes head after head.  A whole step of values is turned round in registers, so that its
+// lines are written whole; of a part of one every element is written on its own.
+// =====================================================================================================
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, const PagedRope rope) {
+  constexpr int PER = Elem<T>::PER, KSTEP = 4 * PER, HALF = DH / 2, LPR = HALF / PER, RPP = WAVE / LPR;   // LPR lanes: a row's pairs
+  typedef T frag __attribute__((ext_vector_type(PER)));
+  __shared__ float2 sm_cs[KSTEP][HALF + 1];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, b = blockIdx.y;
+  const int len = a.seqs.kv_len[b], fresh = a.seqs.n_valid ? paged_new(a.seqs.n_new, a.seqs.n_valid[b]) : a.seqs.n_new;
+  const int L = paged_rows(len, fresh, a.seqs.cap);
+  if (L < 0) {                                         // (whole workgroup)
+    if (tid == 0 && blockIdx.x == 0 && blockIdx.z == 0) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
+    return;
+  }
+  const int step = len / KSTEP + blockIdx.x, row0 = max(step * KSTEP, len), row1 = min((step + 1) * KSTEP, L), live = row1 - row0;
+  if (live <= 0) return;
+  const int psteps = a.c.page_rows / KSTEP, pg = step / psteps;
+  const int id = a.c.table[(size_t)b * a.c.table_pages + pg];
+  if ((unsigned)id >= (unsigned)a.c.n_pages) {
+    if (tid == 0) atomicOr(a.dev_status, (unsigned)AMPH_DEV_BAD_PAGE);
+    return;
+  }
+  const int j0 = row0 - len, k0 = row0 - step * KSTEP;             // the first row among the new ones, and in its step
+  const size_t new0 = (size_t)b * a.seqs.n_new + j0;
+  for (int t = tid; t < live * HALF; t += 256) {
+    const int r = t / HALF, i = t % HALF;
+    // turns, in 64 bits: of a far position's angle 32 bits would leave a few places; then what is left of the last whole turn
+    const double turns = (double)(a.pos ? a.pos[new0 + r] : row0 + r) * rope.turns[i];
+    float sn, cs;
+    sincosf((float)((turns - rint(turns)) * 6.283185307179586), &sn, &cs);
+    sm_cs[r][i] = make_float2(cs, sn);
+  }
+  __syncthreads();
+  const size_t page = (size_t)id * a.c.page_stride + (size_t)(step - pg * psteps) * (KSTEP * DH);
+  const int n_rot = (a.q ? a.n_heads : 0) + a.c.n_kv, n_units = n_rot + a.c.n_kv;
+  for (int unit = blockIdx.z * 4 + wave; unit < n_units; unit += gridDim.z * 4) {
+    const bool is_q = unit < n_rot - a.c.n_kv, is_v = unit >= n_rot;
+    const int h = is_v ? unit - n_rot : is_q ? unit : unit - (n_rot - a.c.n_kv);
+    if (!is_v) {
+      const T *src = (const T *)(is_q ? a.q : a.k) + new0 * (is_q ? a.ld_q : a.ld_k) + (size_t)h * DH;
+      const size_t ld = is_q ? a.ld_q : a.ld_k;
+      T *dst = is_q ? (T *)a.q_out + (new0 * a.n_heads + h) * DH : (T *)a.c.k + page + (size_t)h * a.c.head_stride;
+      const int p = (lane % LPR) * PER;
+      for (int r = lane / LPR; r < live; r += RPP) {
+        const frag lo = *reinterpret_cast<const frag *>(src + r * ld + p), hi = *reinterpret_cast<const frag *>(src + r * ld + HALF + p);
+        frag x, y;
+        #pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const float2 cs = sm_cs[r][p + e];
+          const float u = Elem<T>::to_f32(lo[e]), v = Elem<T>::to_f32(hi[e]);
+          x[e] = Elem<T>::from_f32(u * cs.x - v * cs.y);
+          y[e] = Elem<T>::from_f32(v * cs.x + u * cs.y);
+        }
+        if (is_q) {
+          *reinterpret_cast<frag *>(dst + (size_t)r * a.n_heads * DH + p) = x;
+          *reinterpret_cast<frag *>(dst + (size_t)r * a.n_heads * DH + HALF + p) = y;
+        } else {
+          *reinterpret_cast<frag *>(dst + k_tiled_index<T>(k0 + r, p, DH)) = x;
+          *reinterpret_cast<frag *>(dst + k_tiled_index<T>(k0 + r, HALF + p, DH)) = y;
+        }
+      }
+      if (!is_q && lane < live) {
+        const size_t at = ((size_t)b * a.c.n_kv + h) * a.c.table_pages * a.c.page_rows + row0 + lane;
+        if (a.weights) a.weights[at] = 0.f;
+        if (a.row_pos) a.row_pos[at] = a.pos ? a.pos[new0 + lane] : row0 + lane;
+      }
+    } else {
+      const T *src = (const T *)a.v + new0 * a.ld_v + (size_t)h * DH;
+      T *dst = (T *)a.c.v + page + (size_t)h * a.c.head_stride;
+      if (live == KSTEP) {
+        constexpr int UN = DH / 16, LPV = DH / PER;    // a lane has UN adjacent rows of PER adjacent dims
+        typedef T run __attribute__((ext_vector_type(UN)));
+        const int li = lane % LPV, grp = lane / LPV;
+        frag x[UN];
+        #pragma unroll
+        for (int j = 0; j < UN; ++j) x[j] = *reinterpret_cast<const frag *>(src + (size_t)(grp * UN + j) * a.ld_v + li * PER);
+        #pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          run y;
+          #pragma unroll
+          for (int j = 0; j < UN; ++j) y[j] = x[j][e];
+          *reinterpret_cast<run *>(dst + v_tiled_index<T>(grp * UN, li * PER + e, DH)) = y;
+        }
+      } else {
+        for (int r = 0; r < live; ++r)
+          #pragma unroll
+          for (int c = lane; c < DH; c += WAVE) dst[v_tiled_index<T>(k0 + r, c, DH)] = src[(size_t)r * a.ld_v + c];
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch_paged_append(hipStream_t st, const PagedAppendArgs &a, const PagedRope &rope, int d_h) {
+  constexpr int KSTEP = 4 * Elem<T>::PER;
+  const int steps = (a.seqs.n_new + KSTEP - 2) / KSTEP + 1, units = (a.q ? a.n_heads : 0) + 2 * a.c.n_kv;
+  // heads are spread over workgroups until there are two for every compute unit
+  const long long have = (long long)steps * a.seqs.n_seq;
+  const int z = (int)std::min<long long>((units + 3) / 4, std::max<long long>(1, (512 + have - 1) / have));
+  const dim3 grid(steps, a.seqs.n_seq, z);
+  if (d_h == 128) hipLaunchKernelGGL((k_paged_append<T, 128>), grid, dim3(256), 0, st, a, rope);
+  else hipLaunchKernelGGL((k_paged_append<T, 64>), grid, dim3(256), 0, st, a, rope);
+  return hipGetLastError();
+}
+template hipError_t launch_paged_append<float>(hipStream_t, const PagedAppendArgs &, const PagedRope &, int);
+template hipError_t launch_paged_append<bf16_t>(hipStream_t, const PagedAppendArgs &, const PagedRope &, int);
+
+// =====================================================================================================
+// amph_paged_evict
+// k_evict_select: one workgroup for every (layer, sequence, key head).  Finds the smallest kept key (a row's weight as an ordered
+//   integer, all ones for the newest rows) by four rounds of counting its next eight bits, of equal keys the lowest rows; lists the
+//   dropped rows below the budget and the kept ones behind it, both ascending, and moves weights and positions.
+// k_evict_move: the listed rows' keys and values.  Sources lie behind the budget and destinations below it, so no order is needed.
+// =====================================================================================================
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+
+__global__ __launch_bounds__(256) void k_evict_select(const PagedEvictArgs a) {
+  constexpr int NW = 4;
+  __shared__ int hist[256];
+  __shared__ int sm_a[NW], sm_b[NW], sm_pick[2];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;      // (layer, sequence, key head)
+  const int b = (unit / a.c.n_kv) % a.seqs.n_seq, cap = a.seqs.cap;
+  const bool speaker = unit % a.c.n_kv == 0 && unit / (a.c.n_kv * a.seqs.n_seq) == 0;    // one workgroup of the sequence
+  int R = paged_len(a.seqs, b);
+  bool bad_page = false;
+  for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += 256)
+    bad_page |= (unsigned)a.c.table[(size_t)b * a.c.table_pages + i] >= (unsigned)a.c.n_pages;
+  bad_page = __syncthreads_or(bad_page);
+  if (R < 0 || bad_page) {                             // nothing changes for this sequence
+    if (tid == 0) {
+      a.n_moves[unit] = 0;
+      if (speaker) {
+        a.new_len[b] = a.seqs.kv_len[b];
+        atomicOr(a.dev_status, (unsigned)(R < 0 ? AMPH_DEV_KV_OVERFLOW : AMPH_DEV_BAD_PAGE));
+      }
+    }
+    return;
+  }
+  const size_t at = (size_t)unit * a.c.table_pages * a.c.page_rows;
+  const float *w = a.weights_in + at;
+  const int32_t *pos = a.pos_in + at;
+  float *w_out = a.weights_out + at;
+  int32_t *pos_out = a.pos_out + at;
+  const bool in_place = a.weights_in == a.weights_out && a.pos_in == a.pos_out;
+  if (speaker && tid == 0) a.new_len[b] = min(R, a.budget);
+  if (R <= a.budget) {
+    if (tid == 0) a.n_moves[unit] = 0;
+    if (!in_place)
+      for (int j = tid; j < R; j += 256) { w_out[j] = w[j]; pos_out[j] = pos[j]; }
+    return;
+  }
+  int newest = INT32_MIN;
+  for (int j = tid; j < R; j += 256) newest = max(newest, pos[j]);
+  newest = wave_max(newest);
+  if (lane == 0) sm_a[wave] = newest;
+  __syncthreads();
+  newest = max(max(sm_a[0], sm_a[1]), max(sm_a[2], sm_a[3]));
+  const long long safe_from = (long long)newest - a.recent;           // positions above it are kept first
+  auto key_of = [&](int j) -> unsigned { return (long long)pos[j] > safe_from ? 0xffffffffu : rank_key(w[j]); };
+
+  // ---- the budget-th largest key: `want` of the keys that share the bits found so far are kept
+  unsigned found = 0;
+  int want = a.budget, equal = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < R; j += 256) {
+      const unsigned k = key_of(j);
+      if (shift == 24 || (k >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    // thread t: digit 255 - t; the digit at which the count from the top reaches `want`
+    const int mine = hist[255 - tid];
+    int upto = mine;
+    #pragma unroll
+    for (int o = 1; o < WAVE; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == WAVE - 1) sm_a[wave] = upto;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) upto += sm_a[i];
+    if (upto >= want && upto - mine < want) { sm_pick[0] = 255 - tid; sm_pick[1] = want - (upto - mine); }
+    __syncthreads();
+    found |= (unsigned)sm_pick[0] << shift;
+    want = sm_pick[1];
+    equal = hist[sm_pick[0]];
+    __syncthreads();
+  }
+
+  // ---- rows in order, a run of them for every wave: equal keys before it, then its dropped and kept rows
+  const int per = ((R + NW * WAVE - 1) / (NW * WAVE)) * WAVE, r0 = min(wave * per, R), r1 = min(r0 + per, R);
+  int eq = 0;
+  if (equal > want) {
+    for (int j = r0; j < r1; j += WAVE) eq += __popcll(__ballot(j + lane < r1 && key_of(min(j + lane, R - 1)) == found));
+    if (lane == 0) sm_a[wave] = eq;
+    __syncthreads();
+    eq = 0;
+    for (int i = 0; i < wave; ++i) eq += sm_a[i];
+  } else {
+    eq = INT32_MIN / 2;                                // all of them are kept
+  }
+  const int eq_before = eq;
+  int32_t *holes = a.lists + (size_t)unit * cap, *from = holes + cap / 2;
+  int n_hole = 0, n_from = 0;
+  for (int pass = 0; pass < 2; ++pass) {               // counted, then listed
+    eq = eq_before;
+    for (int j = r0; j < r1; j += WAVE) {
+      const int row = j + lane;
+      const bool in = row < r1;
+      const unsigned k = key_of(min(row, R - 1));
+      const uint64_t same = __ballot(in && k == found);
+      const bool keep = in && (k > found || (k == found && eq + lanes_before(same) < want));
+      eq += __popcll(same);
+      const bool hole = in && !keep && row < a.budget, mover = keep && row >= a.budget;
+      const uint64_t mh = __ballot(hole), mf = __ballot(mover);
+      if (pass) {
+        if (hole) holes[n_hole + lanes_before(mh)] = row;
+        if (mover) from[n_from + lanes_before(mf)] = row;
+        if (!in_place && keep && !mover) { w_out[row] = w[row]; pos_out[row] = pos[row]; }
+      }
+      n_hole += __popcll(mh);
+      n_from += __popcll(mf);
+    }
+    __syncthreads();
+    if (pass == 0) {
+      if (lane == 0) { sm_a[wave] = n_hole; sm_b[wave] = n_from; }
+      __syncthreads();
+      n_hole = n_from = 0;
+      for (int i = 0; i < wave; ++i) { n_hole += sm_a[i]; n_from += sm_b[i]; }
+    }
+  }
+  const int moves = sm_a[0] + sm_a[1] + sm_a[2] + sm_a[3];
+  if (tid == 0) a.n_moves[unit] = moves;
+  for (int i = tid; i < moves; i += 256) {
+    const int d = holes[i], s = from[i];
+    w_out[d] = w[s];
+    pos_out[d] = pos[s];
+  }
+}
+
+constexpr int EVICT_MOVES = 64;                        // moves of a workgroup: 16 a wave
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a) {
+  constexpr int PIECE = 64 / (int)sizeof(T), SEGS = DH / PIECE;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;
+  const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
+  if (h == 0 && layer == 0 && blockIdx.y == 0 && tid == 0) a.kv_len_out[b] = a.new_len[b];
+  const int n = a.n_moves[unit];
+  const int32_t *holes = a.lists + (size_t)unit * a.seqs.cap, *from = holes + a.seqs.cap / 2;
+  const int32_t *row_table = a.c.table + (size_t)b * a.c.table_pages;
+  const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
+  // lane = 16 moves x 4: a quarter of a 64-byte column of the keys, every fourth dim of the values
+  const int m = lane & 15, sub = lane >> 4;
+  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES) {
+    const bool in = i0 + m < n;
+    const int i = min(i0 + m, n - 1), d = holes[i], s = from[i];
+    const int dp = d / a.c.page_rows, sp = s / a.c.page_rows, dr = d - dp * a.c.page_rows, sr = s - sp * a.c.page_rows;
+    const size_t dpage = base + (size_t)row_table[dp] * a.c.page_stride, spage = base + (size_t)row_table[sp] * a.c.page_stride;
+    T *K = (T *)a.c.k, *V = (T *)a.c.v;
+    uint4 k[SEGS];
+    #pragma unroll
+    for (int p = 0; p < SEGS; ++p) k[p] = ldg16(K + spage + k_tiled_index<T>(sr, p * PIECE + sub * (PIECE / 4), DH));
+    #pragma unroll
+    for (int p = 0; p < SEGS; ++p) if (in) stg16(K + dpage + k_tiled_index<T>(dr, p * PIECE + sub * (PIECE / 4), DH), k[p]);
+    constexpr int UN = 16;
+    for (int c0 = 0; c0 < DH; c0 += 4 * UN) {
+      T v[UN];
+      #pragma unroll
+      for (int e = 0; e < UN; ++e) v[e] = V[spage + v_tiled_index<T>(sr, c0 + e * 4 + sub, DH)];
+      #pragma unroll
+      for (int e = 0; e < UN; ++e) if (in) V[dpage + v_tiled_index<T>(dr, c0 + e * 4 + sub, DH)] = v[e];
+    }
+  }
+}
+
+size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, PagedEvictArgs *a, unsigned char *ws) {
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t o = at; at = (at + n + 255) / 256 * 256; return ws ? ws + o : nullptr; };
+  const size_t units = (size_t)n_layers * n_seq * n_kv;
+  unsigned char *len = take((size_t)n_seq * 4), *moves = take(units * 4), *lists = take(units * cap * 4);
+  if (a) { a->new_len = (int32_t *)len; a->n_moves = (int32_t *)moves; a->lists = (int32_t *)lists; }
+  return at;
+}
+
+template <typename T>
+hipError_t launch_paged_evict(hipStream_t st, const PagedEvictArgs &a, int n_layers, int d_h) {
+  const unsigned units = (unsigned)n_layers * a.seqs.n_seq * a.c.n_kv;
+  const int most = std::min(a.budget, std::max(a.seqs.cap - a.budget, 0));
+  hipLaunchKernelGGL(k_evict_select, dim3(units), dim3(256), 0, st, a);
+  const dim3 grid(units, std::min(std::max((most + EVICT_MOVES - 1) / EVICT_MOVES, 1), 65535));
+  if (d_h == 128) hipLaunchKernelGGL((k_evict_move<T, 128>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_evict_move<T, 64>), grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template hipError_t launch_paged_evict<float>(hipStream_t, const PagedEvictArgs &, int, int);
+template hipError_t launch_paged_evict<bf16_t>(hipStream_t, const PagedEvictArgs &, int, int);
+
+}  // namespace amph

@@ -7,7 +7,7 @@ import numpy as np
 import torch
 
 from .binding import (AMPH_BF16, AMPH_F32, AMPH_PACK_DOWN, AMPH_PACK_GATEUP, AMPH_PACK_LMHEAD, AMPH_PACK_QKV,
-                      AMPH_PACK_WO, amph_layer_tiled)
+                      AMPH_PACK_WO, amph_layer_tiled, amph_paged_kv)
 
 
 def dtype_code(name: str) -> int:
@@ -87,3 +87,27 @@ def pack_lm_head(ctx, lm_head: torch.Tensor) -> torch.Tensor:
     out = torch.empty(ctx.amph_tiled_bytes(AMPH_PACK_LMHEAD), dtype=torch.uint8, device=lm_head.device)
     ctx.amph_pack_weights(AMPH_PACK_LMHEAD, lm_head, None, None, out)
     return out
+
+
+def paged_pool(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, max_pages: int | None = None) -> amph_paged_kv:
+    """A pool of pages [n_layers, n_pages, n_kv_heads, page_rows, head_dim] (step-tiled) and its table [n_seq, table_pages] int32 as the
+    paged calls take them.  The caller keeps the tensors alive as long as the struct is used."""
+    assert k_pages.shape == v_pages.shape and k_pages.dim() == 5 and k_pages.is_contiguous() and v_pages.is_contiguous()
+    assert k_pages.dtype == v_pages.dtype and table.dtype == torch.int32 and table.dim() == 2 and table.is_contiguous()
+    _, n_pages, n_kv, rows, d_h = k_pages.shape
+    page = rows * d_h
+    return amph_paged_kv(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), table.shape[0], n_kv, rows, n_pages, table.shape[1],
+                         table.shape[1] if max_pages is None else max_pages, n_kv * page, page, n_pages * n_kv * page)
+
+
+def paged_caches(k_caches: torch.Tensor, v_caches: torch.Tensor, page_rows: int):
+    """The caches of amph_target_forward, [n_layers, B, n_heads, max_kv, head_dim] (step-tiled), as pages of page_rows rows where they
+    lie.  Returns (amph_paged_kv, table): the caller keeps the table and the caches alive as long as the struct is used."""
+    assert k_caches.shape == v_caches.shape and k_caches.dim() == 5 and k_caches.is_contiguous() and v_caches.is_contiguous()
+    assert k_caches.dtype == v_caches.dtype and k_caches.shape[3] % page_rows == 0
+    _, batch, n_h, max_kv, d_h = k_caches.shape
+    per = max_kv // page_rows
+    first = torch.arange(batch, dtype=torch.int32, device=k_caches.device) * (n_h * per)
+    table = (first[:, None] + torch.arange(per, dtype=torch.int32, device=k_caches.device)).contiguous()
+    return amph_paged_kv(k_caches.data_ptr(), v_caches.data_ptr(), table.data_ptr(), batch, n_h, page_rows, batch * n_h * per, per, per,
+                         page_rows * d_h, max_kv * d_h, batch * n_h * max_kv * d_h), table

@@ -832,7 +832,7 @@ amph_status amph_paged_bytes(amph_ctx *ctx, const amph_paged_kv *kv, int n_layer
   if (amph_status s = check_paged(ctx, kv, n_layers, "amph_paged_bytes")) return s;
   const int cap = kv->max_pages * kv->page_rows;
   *bytes = paged_attn_ws_bytes(kv->n_seq, ctx->cfg.n_heads, kv->n_kv_heads, ctx->cfg.head_dim, cap, n_layers > 0, nullptr, nullptr);
-  if (n_layers > 0) *bytes = std::max(*bytes, paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, cap, nullptr, nullptr));
+  if (n_layers > 0) *bytes = std::max(*bytes, paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, cap, 0, nullptr, nullptr));
   return AMPH_OK;
 }
 
@@ -903,7 +903,7 @@ amph_status amph_paged_evict(amph_ctx *ctx, const amph_paged_kv *kv, int n_layer
   a.c = paged_pages(ctx, kv, 0); a.seqs = paged_seqs(kv, n_new, n_valid, kv_len);
   a.budget = budget; a.recent = recent; a.weights_in = weights_in; a.weights_out = weights_out; a.pos_in = row_pos_in;
   a.pos_out = row_pos_out; a.kv_len_out = kv_len_out; a.dev_status = ctx->dev_status;
-  paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, a.seqs.cap, &a, (unsigned char *)workspace);
+  paged_evict_ws_bytes(n_layers, kv->n_seq, kv->n_kv_heads, a.seqs.cap, budget, &a, (unsigned char *)workspace);
   if (ctx->cfg.dtype == AMPH_BF16) HIP_TRY(ctx, launch_paged_evict<bf16_t>(ctx->stream, a, n_layers, ctx->cfg.head_dim));
   else HIP_TRY(ctx, launch_paged_evict<float>(ctx->stream, a, n_layers, ctx->cfg.head_dim));
   return AMPH_OK;

@@ -222,9 +222,10 @@ struct PagedEvictArgs {
   const float *weights_in; float *weights_out;
   const int32_t *pos_in; int32_t *pos_out, *kv_len_out;
   uint32_t *dev_status;
-  int32_t *new_len, *n_moves, *lists;                             // in the workspace: paged_evict_ws_bytes
+  int32_t *new_len, *n_moves; int2 *moves; int most;              // in the workspace: paged_evict_ws_bytes; up to `most` moves a head
+  bool fused;                                                     // the workgroup that chooses rows moves them too
 };
-size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, PagedEvictArgs *a, unsigned char *ws);
+size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, int budget, PagedEvictArgs *a, unsigned char *ws);
 template <typename T> hipError_t launch_paged_evict(hipStream_t st, const PagedEvictArgs &a, int n_layers, int d_h);
 
 }  // namespace amph

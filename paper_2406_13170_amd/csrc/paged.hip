@@ -603,194 +603,338 @@ template hipError_t launch_paged_append<bf16_t>(hipStream_t, const PagedAppendAr
 
 // =====================================================================================================
 // amph_paged_evict
-// k_evict_select: one workgroup for every (layer, sequence, key head).  Finds the smallest kept key (a row's weight as an ordered
-//   integer, all ones for the newest rows) by four rounds of counting its next eight bits, of equal keys the lowest rows; lists the
-//   dropped rows below the budget and the kept ones behind it, both ascending, and moves weights and positions.
-// k_evict_move: the listed rows' keys and values.  Sources lie behind the budget and destinations below it, so no order is needed.
+// k_evict: one workgroup for every (layer, sequence, key head).  A row's key is its weight as an ordered integer, all ones for the
+//   newest rows.  The smallest kept key is found by counting: the range from the smallest to the largest key in 2048 bins, then
+//   the bin that holds it the same way (spread over the range, the counters are hit by few lanes at once, however close the
+//   exponents are).  Then the rows in their order: of equal keys the lowest are kept, the i-th kept row behind the budget gets the
+//   i-th dropped place below it.  A step that drops one row (a cache at its budget) needs only the smallest key.
+// The keys and values of the moved rows: by the same workgroup where few can move, or k_evict_move with workgroups for every
+// 64 moves.  Sources lie behind the budget and destinations below it, so no order is needed.
 // =====================================================================================================
 __device__ __forceinline__ int lanes_before(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
+struct MinU { __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return min(a, b); } };
+struct MaxU { __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); } };
+struct AddI { __device__ __forceinline__ int operator()(int a, int b) const { return a + b; } };
 
-__global__ __launch_bounds__(256) void k_evict_select(const PagedEvictArgs a) {
-  constexpr int NW = 4;
-  __shared__ int hist[256];
-  __shared__ int sm_a[NW], sm_b[NW], sm_pick[2];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;      // (layer, sequence, key head)
-  const int b = (unit / a.c.n_kv) % a.seqs.n_seq, cap = a.seqs.cap;
-  const bool speaker = unit % a.c.n_kv == 0 && unit / (a.c.n_kv * a.seqs.n_seq) == 0;    // one workgroup of the sequence
-  int R = paged_len(a.seqs, b);
-  bool bad_page = false;
-  for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += 256)
-    bad_page |= (unsigned)a.c.table[(size_t)b * a.c.table_pages + i] >= (unsigned)a.c.n_pages;
-  bad_page = __syncthreads_or(bad_page);
-  if (R < 0 || bad_page) {                             // nothing changes for this sequence
-    if (tid == 0) {
-      a.n_moves[unit] = 0;
-      if (speaker) {
-        a.new_len[b] = a.seqs.kv_len[b];
-        atomicOr(a.dev_status, (unsigned)(R < 0 ? AMPH_DEV_KV_OVERFLOW : AMPH_DEV_BAD_PAGE));
-      }
+// Rows s[m] -> d[m] of one head for the 16 moves i0 .. i0 + 15 (of n), by one wave: lane = 16 moves x 4; a quarter of a 64-byte column
+// of the keys, every fourth dim of the values.
+template <typename T, int DH>
+__device__ __forceinline__ void evict_move_rows(const PagedPages &c, const int32_t *row_table, size_t base, const int2 *moves, int i0, int n) {
+  constexpr int PIECE = 64 / (int)sizeof(T), SEGS = DH / PIECE;
+  const int lane = threadIdx.x & 63, m = lane & 15, sub = lane >> 4;
+  const bool in = i0 + m < n;
+  const int2 mv = moves[min(i0 + m, n - 1)];
+  const int d = mv.x, s = mv.y, dp = d / c.page_rows, sp = s / c.page_rows, dr = d - dp * c.page_rows, sr = s - sp * c.page_rows;
+  const size_t dpage = base + (size_t)row_table[dp] * c.page_stride, spage = base + (size_t)row_table[sp] * c.page_stride;
+  T *K = (T *)c.k, *V = (T *)c.v;
+  uint4 k[SEGS];
+  #pragma unroll
+  for (int p = 0; p < SEGS; ++p) k[p] = ldg16(K + spage + k_tiled_index<T>(sr, p * PIECE + sub * (PIECE / 4), DH));
+  constexpr int UN = 16;
+  #pragma unroll
+  for (int c0 = 0; c0 < DH; c0 += 4 * UN) {
+    T v[UN];
+    #pragma unroll
+    for (int e = 0; e < UN; ++e) if (c0 + e * 4 < DH) v[e] = V[spage + v_tiled_index<T>(sr, c0 + e * 4 + sub, DH)];
+    if (in) {
+      #pragma unroll
+      for (int e = 0; e < UN; ++e) if (c0 + e * 4 < DH) V[dpage + v_tiled_index<T>(dr, c0 + e * 4 + sub, DH)] = v[e];
     }
-    return;
   }
+  if (in) {
+    #pragma unroll
+    for (int p = 0; p < SEGS; ++p) stg16(K + dpage + k_tiled_index<T>(dr, p * PIECE + sub * (PIECE / 4), DH), k[p]);
+  }
+}
+
+// NT threads; RPT > 0: a thread keeps its RPT rows' weights and positions in registers (cap <= NT * RPT), 0: they are read anew.
+template <typename T, int DH, int NT, int RPT>
+__global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
+  constexpr int NW = NT / WAVE, BINS = 2048;
+  constexpr bool HELD = RPT > 0;
+  extern __shared__ int sm_hole[];                     // [most moves] places below the budget, ascending (HELD)
+  __shared__ int hist[BINS], sm_a[NW], sm_b[NW], sm_c[NW], sm_pick[3];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, unit = blockIdx.x;
+  const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
+  const bool speaker = h == 0 && layer == 0 && tid == 0;                                  // one thread of the sequence
   const size_t at = (size_t)unit * a.c.table_pages * a.c.page_rows;
   const float *w = a.weights_in + at;
-  const int32_t *pos = a.pos_in + at;
+  const int32_t *pos = a.pos_in + at, *row_table = a.c.table + (size_t)b * a.c.table_pages;
   float *w_out = a.weights_out + at;
   int32_t *pos_out = a.pos_out + at;
   const bool in_place = a.weights_in == a.weights_out && a.pos_in == a.pos_out;
-  if (speaker && tid == 0) a.new_len[b] = min(R, a.budget);
-  if (R <= a.budget) {
-    if (tid == 0) a.n_moves[unit] = 0;
-    if (!in_place)
-      for (int j = tid; j < R; j += 256) { w_out[j] = w[j]; pos_out[j] = pos[j]; }
-    return;
+  const int len = a.seqs.kv_len[b], R = paged_len(a.seqs, b), budget = a.budget;
+
+  // ---- a run of rows for every wave: row r0 + 64 i + lane
+  const int per = ((max(R, 0) + NT - 1) / NT) * WAVE, r0 = wave * per, r1 = min(r0 + per, R);
+  float wr[HELD ? RPT : 1];
+  int pr[HELD ? RPT : 1];
+  if constexpr (HELD) {
+    #pragma unroll
+    for (int i = 0; i < RPT; ++i) {                    // (all of them at once; rows that are none re-read one that may be any place of the buffer)
+      const int row = min(r0 + i * WAVE + lane, max(R - 1, 0));
+      wr[i] = w[row];
+      pr[i] = pos[row];
+    }
   }
+  bool bad = R < 0;
+  for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += NT) bad |= (unsigned)row_table[i] >= (unsigned)a.c.n_pages;
+  auto rows = [&](auto f) {                            // f(row, is one, weight, position), a row a lane
+    if constexpr (HELD) {
+      #pragma unroll
+      for (int i = 0; i < RPT; ++i) f(r0 + i * WAVE + lane, r0 + i * WAVE + lane < r1, wr[i], pr[i]);
+    } else {
+      for (int j = r0; j < r1; j += WAVE) {
+        const int row = min(j + lane, R - 1);
+        f(j + lane, j + lane < r1, w[row], pos[row]);
+      }
+    }
+  };
   int newest = INT32_MIN;
-  for (int j = tid; j < R; j += 256) newest = max(newest, pos[j]);
+  rows([&](int, bool in, float, int p) { if (in) newest = max(newest, p); });
   newest = wave_max(newest);
   if (lane == 0) sm_a[wave] = newest;
-  __syncthreads();
-  newest = max(max(sm_a[0], sm_a[1]), max(sm_a[2], sm_a[3]));
+  bad = __syncthreads_or(bad);
+  if (speaker) {
+    const int now = bad ? len : min(R, budget);        // nothing changes for a sequence that is not sound
+    if (a.kv_len_out) a.kv_len_out[b] = now; else a.new_len[b] = now;
+    if (bad) atomicOr(a.dev_status, (unsigned)(R < 0 ? AMPH_DEV_KV_OVERFLOW : AMPH_DEV_BAD_PAGE));
+  }
+  if (bad || R <= budget) {
+    if (!a.fused && tid == 0) a.n_moves[unit] = 0;
+    if (!bad && !in_place) rows([&](int row, bool in, float x, int p) { if (in) { w_out[row] = x; pos_out[row] = p; } });
+    return;
+  }
+  #pragma unroll
+  for (int i = 0; i < NW; ++i) newest = max(newest, sm_a[i]);
   const long long safe_from = (long long)newest - a.recent;           // positions above it are kept first
-  auto key_of = [&](int j) -> unsigned { return (long long)pos[j] > safe_from ? 0xffffffffu : rank_key(w[j]); };
+  auto key_of = [&](float x, int p) -> unsigned { return (long long)p > safe_from ? 0xffffffffu : rank_key(x); };
+  int2 *moves = a.moves + (size_t)unit * a.most;
+  const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
 
-  // ---- the budget-th largest key: `want` of the keys that share the bits found so far are kept
-  unsigned found = 0;
-  int want = a.budget, equal = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
+  if (R == budget + 1) {
+    // ---- the smallest key goes, the last row of that key
+    unsigned least = 0xffffffffu;
+    rows([&](int, bool in, float x, int p) { if (in) least = min(least, key_of(x, p)); });
+    least = wave_fold(least, MinU());
+    if (lane == 0) sm_b[wave] = (int)least;
     __syncthreads();
-    for (int j = tid; j < R; j += 256) {
-      const unsigned k = key_of(j);
-      if (shift == 24 || (k >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
-    }
-    __syncthreads();
-    // thread t: digit 255 - t; the digit at which the count from the top reaches `want`
-    const int mine = hist[255 - tid];
-    int upto = mine;
     #pragma unroll
-    for (int o = 1; o < WAVE; o <<= 1) {
-      const int v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
+    for (int i = 0; i < NW; ++i) least = min(least, (unsigned)sm_b[i]);
+    int gone = -1;
+    rows([&](int row, bool in, float x, int p) { if (in && key_of(x, p) == least) gone = max(gone, row); });
+    gone = wave_max(gone);
+    if (lane == 0) sm_c[wave] = gone;
+    __syncthreads();
+    #pragma unroll
+    for (int i = 0; i < NW; ++i) gone = max(gone, sm_c[i]);
+    rows([&](int row, bool in, float x, int p) {
+      if (in && row == budget && gone < budget) { w_out[gone] = x; pos_out[gone] = p; }
+      else if (in && !in_place && row < budget && row != gone) { w_out[row] = x; pos_out[row] = p; }
+    });
+    const int2 one = make_int2(gone, budget);
+    if (!a.fused) {
+      if (tid == 0) { moves[0] = one; a.n_moves[unit] = gone < budget; }
+    } else if (wave == 0 && gone < budget) {
+      evict_move_rows<T, DH>(a.c, row_table, base, &one, 0, 1);
     }
-    if (lane == WAVE - 1) sm_a[wave] = upto;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) upto += sm_a[i];
-    if (upto >= want && upto - mine < want) { sm_pick[0] = 255 - tid; sm_pick[1] = want - (upto - mine); }
-    __syncthreads();
-    found |= (unsigned)sm_pick[0] << shift;
-    want = sm_pick[1];
-    equal = hist[sm_pick[0]];
-    __syncthreads();
+    return;
   }
 
-  // ---- rows in order, a run of them for every wave: equal keys before it, then its dropped and kept rows
-  const int per = ((R + NW * WAVE - 1) / (NW * WAVE)) * WAVE, r0 = min(wave * per, R), r1 = min(r0 + per, R);
+  // ---- the smallest kept key among those that are no newest row's: `want` of the keys in [lo, hi] are kept
+  unsigned lo = 0xffffffffu, hi = 0u;
+  int safe = 0;
+  rows([&](int, bool in, float x, int p) {
+    const unsigned k = key_of(x, p);
+    const bool fixed = k == 0xffffffffu;
+    safe += __popcll(__ballot(in && fixed));
+    if (in && !fixed) { lo = min(lo, k); hi = max(hi, k); }
+  });
+  lo = wave_fold(lo, MinU());
+  hi = wave_fold(hi, MaxU());
+  __syncthreads();                                     // (sm_a is read)
+  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; }
+  for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+  __syncthreads();
+  safe = 0;
+  #pragma unroll
+  for (int i = 0; i < NW; ++i) { safe += sm_a[i]; lo = min(lo, (unsigned)sm_b[i]); hi = max(hi, (unsigned)sm_c[i]); }
+  int want = budget - safe, equal;
+  if (want <= 0) { lo = 0xffffffffu; want = budget; equal = safe; }
+  else {
+    for (;;) {
+      const unsigned span = hi - lo;
+      const int shift = span >> 11 ? 21 - __clz(span) : 0;             // (bins: span >> shift < 2048)
+      rows([&](int, bool in, float x, int p) {
+        const unsigned k = key_of(x, p);
+        if (in && k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+      });
+      __syncthreads();
+      // from the top, thread t has PB bins; the bin at which the count reaches `want`
+      constexpr int PB = BINS / NT;
+      int c[PB], mine = 0;
+      #pragma unroll
+      for (int i = 0; i < PB; ++i) { c[i] = hist[BINS - 1 - (tid * PB + i)]; mine += c[i]; }
+      int upto = mine;
+      #pragma unroll
+      for (int o = 1; o < WAVE; o <<= 1) {
+        const int v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (lane == WAVE - 1) sm_a[wave] = upto;
+      __syncthreads();
+      #pragma unroll
+      for (int i = 0; i < PB; ++i) hist[BINS - 1 - (tid * PB + i)] = 0;
+      for (int i = 0; i < wave; ++i) upto += sm_a[i];
+      int above = upto - mine;
+      if (upto >= want && above < want) {
+        #pragma unroll
+        for (int i = 0; i < PB; ++i) {
+          if (above < want && above + c[i] >= want) { sm_pick[0] = BINS - 1 - (tid * PB + i); sm_pick[1] = want - above; sm_pick[2] = c[i]; above = want; }
+          else if (above < want) above += c[i];
+        }
+      }
+      __syncthreads();
+      lo += (unsigned)sm_pick[0] << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      want = sm_pick[1];
+      equal = sm_pick[2];
+      if (shift == 0 || equal == want) break;          // one key; or all of the bin is kept
+    }
+  }
+  // kept: above hi; in [lo, hi] (one key, where not all are kept) the first `want`
+  const unsigned from_key = lo;
+  const bool all_equal = equal == want;
   int eq = 0;
-  if (equal > want) {
-    for (int j = r0; j < r1; j += WAVE) eq += __popcll(__ballot(j + lane < r1 && key_of(min(j + lane, R - 1)) == found));
-    if (lane == 0) sm_a[wave] = eq;
+  if (!all_equal) {
+    rows([&](int, bool in, float x, int p) { eq += __popcll(__ballot(in && key_of(x, p) == from_key)); });
+    if (lane == 0) sm_b[wave] = eq;
     __syncthreads();
     eq = 0;
-    for (int i = 0; i < wave; ++i) eq += sm_a[i];
-  } else {
-    eq = INT32_MIN / 2;                                // all of them are kept
+    for (int i = 0; i < wave; ++i) eq += sm_b[i];
   }
   const int eq_before = eq;
-  int32_t *holes = a.lists + (size_t)unit * cap, *from = holes + cap / 2;
+  auto kept = [&](bool in, unsigned k) {
+    if (all_equal) return in && k >= from_key;
+    const uint64_t same = __ballot(in && k == from_key);
+    const bool keep = in && (k > from_key || (k == from_key && eq + lanes_before(same) < want));
+    eq += __popcll(same);
+    return keep;
+  };
   int n_hole = 0, n_from = 0;
-  for (int pass = 0; pass < 2; ++pass) {               // counted, then listed
-    eq = eq_before;
-    for (int j = r0; j < r1; j += WAVE) {
-      const int row = j + lane;
-      const bool in = row < r1;
-      const unsigned k = key_of(min(row, R - 1));
-      const uint64_t same = __ballot(in && k == found);
-      const bool keep = in && (k > found || (k == found && eq + lanes_before(same) < want));
-      eq += __popcll(same);
-      const bool hole = in && !keep && row < a.budget, mover = keep && row >= a.budget;
-      const uint64_t mh = __ballot(hole), mf = __ballot(mover);
-      if (pass) {
-        if (hole) holes[n_hole + lanes_before(mh)] = row;
-        if (mover) from[n_from + lanes_before(mf)] = row;
-        if (!in_place && keep && !mover) { w_out[row] = w[row]; pos_out[row] = pos[row]; }
+  rows([&](int row, bool in, float x, int p) {
+    const bool keep = kept(in, key_of(x, p));
+    n_hole += __popcll(__ballot(in && !keep && row < budget));
+    n_from += __popcll(__ballot(keep && row >= budget));
+  });
+  __syncthreads();                                     // (sm_a is read)
+  if (lane == 0) { sm_a[wave] = n_hole; sm_c[wave] = n_from; }
+  __syncthreads();
+  int total = 0;
+  n_hole = n_from = 0;
+  for (int i = 0; i < NW; ++i) {
+    if (i < wave) { n_hole += sm_a[i]; n_from += sm_c[i]; }
+    total += sm_a[i];
+  }
+  eq = eq_before;
+  rows([&](int row, bool in, float x, int p) {
+    const bool keep = kept(in, key_of(x, p)), hole = in && !keep && row < budget;
+    const uint64_t mh = __ballot(hole);
+    if (hole) {
+      const int i = n_hole + lanes_before(mh);
+      if constexpr (HELD) sm_hole[i] = row; else moves[i].x = row;
+    }
+    n_hole += __popcll(mh);
+    if (keep && row < budget && !in_place) { w_out[row] = x; pos_out[row] = p; }
+  });
+  __syncthreads();
+  eq = eq_before;
+  rows([&](int row, bool in, float x, int p) {
+    const bool keep = kept(in, key_of(x, p)), mover = keep && row >= budget;
+    const uint64_t mf = __ballot(mover);
+    if (mover) {
+      const int i = n_from + lanes_before(mf);
+      if constexpr (HELD) {
+        const int d = sm_hole[i];
+        moves[i] = make_int2(d, row);
+        w_out[d] = x;
+        pos_out[d] = p;
+      } else {
+        moves[i].y = row;
       }
-      n_hole += __popcll(mh);
-      n_from += __popcll(mf);
     }
+    n_from += __popcll(mf);
+  });
+  if constexpr (!HELD) {                               // (in place the weights change only when nobody reads them any more)
     __syncthreads();
-    if (pass == 0) {
-      if (lane == 0) { sm_a[wave] = n_hole; sm_b[wave] = n_from; }
-      __syncthreads();
-      n_hole = n_from = 0;
-      for (int i = 0; i < wave; ++i) { n_hole += sm_a[i]; n_from += sm_b[i]; }
+    for (int i = tid; i < total; i += NT) {
+      const int2 mv = moves[i];
+      w_out[mv.x] = w[mv.y];
+      pos_out[mv.x] = pos[mv.y];
     }
   }
-  const int moves = sm_a[0] + sm_a[1] + sm_a[2] + sm_a[3];
-  if (tid == 0) a.n_moves[unit] = moves;
-  for (int i = tid; i < moves; i += 256) {
-    const int d = holes[i], s = from[i];
-    w_out[d] = w[s];
-    pos_out[d] = pos[s];
+  if (!a.fused) {
+    if (tid == 0) a.n_moves[unit] = total;
+    return;
   }
+  __syncthreads();
+  for (int i0 = wave * 16; i0 < total; i0 += NW * 16) evict_move_rows<T, DH>(a.c, row_table, base, moves, i0, total);
 }
 
 constexpr int EVICT_MOVES = 64;                        // moves of a workgroup: 16 a wave
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a) {
-  constexpr int PIECE = 64 / (int)sizeof(T), SEGS = DH / PIECE;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;
+__global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a, int32_t *kv_len_out) {
+  const int tid = threadIdx.x, wave = tid >> 6, unit = blockIdx.x;
   const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
-  if (h == 0 && layer == 0 && blockIdx.y == 0 && tid == 0) a.kv_len_out[b] = a.new_len[b];
+  if (!a.kv_len_out && h == 0 && layer == 0 && blockIdx.y == 0 && tid == 0) kv_len_out[b] = a.new_len[b];
+  if (a.fused) return;
   const int n = a.n_moves[unit];
-  const int32_t *holes = a.lists + (size_t)unit * a.seqs.cap, *from = holes + a.seqs.cap / 2;
-  const int32_t *row_table = a.c.table + (size_t)b * a.c.table_pages;
   const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
-  // lane = 16 moves x 4: a quarter of a 64-byte column of the keys, every fourth dim of the values
-  const int m = lane & 15, sub = lane >> 4;
-  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES) {
-    const bool in = i0 + m < n;
-    const int i = min(i0 + m, n - 1), d = holes[i], s = from[i];
-    const int dp = d / a.c.page_rows, sp = s / a.c.page_rows, dr = d - dp * a.c.page_rows, sr = s - sp * a.c.page_rows;
-    const size_t dpage = base + (size_t)row_table[dp] * a.c.page_stride, spage = base + (size_t)row_table[sp] * a.c.page_stride;
-    T *K = (T *)a.c.k, *V = (T *)a.c.v;
-    uint4 k[SEGS];
-    #pragma unroll
-    for (int p = 0; p < SEGS; ++p) k[p] = ldg16(K + spage + k_tiled_index<T>(sr, p * PIECE + sub * (PIECE / 4), DH));
-    #pragma unroll
-    for (int p = 0; p < SEGS; ++p) if (in) stg16(K + dpage + k_tiled_index<T>(dr, p * PIECE + sub * (PIECE / 4), DH), k[p]);
-    constexpr int UN = 16;
-    for (int c0 = 0; c0 < DH; c0 += 4 * UN) {
-      T v[UN];
-      #pragma unroll
-      for (int e = 0; e < UN; ++e) v[e] = V[spage + v_tiled_index<T>(sr, c0 + e * 4 + sub, DH)];
-      #pragma unroll
-      for (int e = 0; e < UN; ++e) if (in) V[dpage + v_tiled_index<T>(dr, c0 + e * 4 + sub, DH)] = v[e];
-    }
-  }
+  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES)
+    evict_move_rows<T, DH>(a.c, a.c.table + (size_t)b * a.c.table_pages, base, a.moves + (size_t)unit * a.most, i0, n);
 }
 
-size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, PagedEvictArgs *a, unsigned char *ws) {
+// Up to so many moves a head the workgroup that chose them makes them itself.
+constexpr int EVICT_FUSED = 256;
+
+size_t paged_evict_ws_bytes(int n_layers, int n_seq, int n_kv, int cap, int budget, PagedEvictArgs *a, unsigned char *ws) {
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at = (at + n + 255) / 256 * 256; return ws ? ws + o : nullptr; };
   const size_t units = (size_t)n_layers * n_seq * n_kv;
-  unsigned char *len = take((size_t)n_seq * 4), *moves = take(units * 4), *lists = take(units * cap * 4);
-  if (a) { a->new_len = (int32_t *)len; a->n_moves = (int32_t *)moves; a->lists = (int32_t *)lists; }
+  const int most = budget ? std::max(std::min(budget, cap - budget), 1) : cap / 2;       // (budget 0: whatever it will be)
+  unsigned char *len = take((size_t)n_seq * 4), *n_moves = take(units * 4), *moves = take(units * most * 8);
+  if (a) { a->new_len = (int32_t *)len; a->n_moves = (int32_t *)n_moves; a->moves = (int2 *)moves; a->most = most; }
   return at;
+}
+
+template <typename T, int DH>
+static hipError_t paged_evict_shape(hipStream_t st, PagedEvictArgs a, int n_layers) {
+  const unsigned units = (unsigned)n_layers * a.seqs.n_seq * a.c.n_kv;
+  int32_t *const len_out = a.kv_len_out;
+  const bool same_len = len_out == a.seqs.kv_len;      // other workgroups may still read it: a launch behind this one writes it
+  if (same_len) a.kv_len_out = nullptr;
+  a.fused = a.most <= EVICT_FUSED;
+  const int cap = a.seqs.cap;
+  const size_t lds = (size_t)a.most * 4;
+  #define EVICT(NT, RPT) hipLaunchKernelGGL((k_evict<T, DH, NT, RPT>), dim3(units), dim3(NT), RPT ? lds : 0, st, a)
+  if (cap <= 512) EVICT(256, 2);
+  else if (cap <= 2048) EVICT(256, 8);
+  else if (cap <= 8192) EVICT(1024, 8);
+  else if (cap <= 16384) EVICT(1024, 16);
+  else EVICT(1024, 0);
+  #undef EVICT
+  if (!a.fused || same_len)
+    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(units, a.fused ? 1 : std::min((a.most + EVICT_MOVES - 1) / EVICT_MOVES, 65535)), dim3(256), 0, st, a,
+                       len_out);
+  return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_paged_evict(hipStream_t st, const PagedEvictArgs &a, int n_layers, int d_h) {
-  const unsigned units = (unsigned)n_layers * a.seqs.n_seq * a.c.n_kv;
-  const int most = std::min(a.budget, std::max(a.seqs.cap - a.budget, 0));
-  hipLaunchKernelGGL(k_evict_select, dim3(units), dim3(256), 0, st, a);
-  const dim3 grid(units, std::min(std::max((most + EVICT_MOVES - 1) / EVICT_MOVES, 1), 65535));
-  if (d_h == 128) hipLaunchKernelGGL((k_evict_move<T, 128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_evict_move<T, 64>), grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return d_h == 128 ? paged_evict_shape<T, 128>(st, a, n_layers) : paged_evict_shape<T, 64>(st, a, n_layers);
 }
 template hipError_t launch_paged_evict<float>(hipStream_t, const PagedEvictArgs &, int, int);
 template hipError_t launch_paged_evict<bf16_t>(hipStream_t, const PagedEvictArgs &, int, int);

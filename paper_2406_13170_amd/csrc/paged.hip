@@ -649,92 +649,142 @@ __device__ __forceinline__ void evict_move_rows(const PagedPages &c, const int32
   }
 }
 
-// NT threads; RPT > 0: a thread keeps its RPT rows' weights and positions in registers (cap <= NT * RPT), 0: they are read anew.
+// Inclusive sum over the lanes of a wave, inside the vector ALU: shifts within rows of 16, then the rows' last lanes passed on.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
+  return v;
+}
+
+// NT threads.  Rows are dealt in order to waves, groups, lanes, J to a lane; RPT > 0: a lane keeps the keys of its RPT rows in registers
+// (cap <= NT * RPT), 0: they are computed anew where they are needed.
 template <typename T, int DH, int NT, int RPT>
 __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
-  constexpr int NW = NT / WAVE, BINS = 2048;
+  constexpr int NW = NT / WAVE, BINS = 2048, FEW = 64;
   constexpr bool HELD = RPT > 0;
-  extern __shared__ int sm_hole[];                     // [most moves] places below the budget, ascending (HELD)
-  __shared__ int hist[BINS], sm_a[NW], sm_b[NW], sm_c[NW], sm_pick[3];
+  constexpr int J = HELD && RPT < 8 ? RPT : 8, GROUPS = HELD ? RPT / J : 1;
+  typedef float fj __attribute__((ext_vector_type(J), aligned(4)));
+  typedef int ij __attribute__((ext_vector_type(J), aligned(4)));
+  extern __shared__ __align__(16) int sm_hole[];       // [most] places below the budget, ascending; [most] moves where they are made here (HELD)
+  __shared__ int hist[BINS];
+  __shared__ __align__(16) int sm_new[NW], sm_a[NW], sm_b[NW], sm_c[NW], sm_d[NW], sm_e[NW];
+  __shared__ int sm_pick[3], sm_few;
+  __shared__ unsigned sm_key[FEW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, unit = blockIdx.x;
   const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
-  const bool speaker = h == 0 && layer == 0 && tid == 0;                                  // one thread of the sequence
   const size_t at = (size_t)unit * a.c.table_pages * a.c.page_rows;
   const float *w = a.weights_in + at;
   const int32_t *pos = a.pos_in + at, *row_table = a.c.table + (size_t)b * a.c.table_pages;
   float *w_out = a.weights_out + at;
   int32_t *pos_out = a.pos_out + at;
-  const bool in_place = a.weights_in == a.weights_out && a.pos_in == a.pos_out;
   const int len = a.seqs.kv_len[b], R = paged_len(a.seqs, b), budget = a.budget;
-
-  // ---- a run of rows for every wave: row r0 + 64 i + lane
-  const int per = ((max(R, 0) + NT - 1) / NT) * WAVE, r0 = wave * per, r1 = min(r0 + per, R);
-  float wr[HELD ? RPT : 1];
-  int pr[HELD ? RPT : 1];
+  const int groups = HELD ? GROUPS : (max(R, 0) + NT * J - 1) / (NT * J);
+  auto row_of = [&](int g) { return (wave * groups + g) * (WAVE * J) + lane * J; };
+  auto load = [&](int g, fj &x, ij &p) {               // (J rows lie in cap places or behind them, as cap is a multiple of J)
+    const int r = min(row_of(g), a.seqs.cap - J);
+    x = *reinterpret_cast<const fj *>(w + r);
+    p = *reinterpret_cast<const ij *>(pos + r);
+  };
+  fj wr[GROUPS];
+  ij pr[GROUPS];
+  const int live_groups = R <= 0 ? 0 : min(groups, (R - 1 - wave * groups * WAVE * J + WAVE * J) / (WAVE * J));      // (may be negative)
   if constexpr (HELD) {
     #pragma unroll
-    for (int i = 0; i < RPT; ++i) {                    // (all of them at once; rows that are none re-read one that may be any place of the buffer)
-      const int row = min(r0 + i * WAVE + lane, max(R - 1, 0));
-      wr[i] = w[row];
-      pr[i] = pos[row];
-    }
+    for (int g = 0; g < GROUPS; ++g) if (g < live_groups) load(g, wr[g], pr[g]);
   }
+  for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+  if (tid == 0) sm_few = 0;
   bool bad = R < 0;
   for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += NT) bad |= (unsigned)row_table[i] >= (unsigned)a.c.n_pages;
-  auto rows = [&](auto f) {                            // f(row, is one, weight, position), a row a lane
+  auto lines = [&](auto f) {                           // f(g, first row of the lane, J weights, J positions)
     if constexpr (HELD) {
       #pragma unroll
-      for (int i = 0; i < RPT; ++i) f(r0 + i * WAVE + lane, r0 + i * WAVE + lane < r1, wr[i], pr[i]);
+      for (int g = 0; g < GROUPS; ++g) if (g < live_groups) f(g, row_of(g), wr[g], pr[g]);
     } else {
-      for (int j = r0; j < r1; j += WAVE) {
-        const int row = min(j + lane, R - 1);
-        f(j + lane, j + lane < r1, w[row], pos[row]);
+      for (int g = 0; g < live_groups; ++g) {
+        fj x;
+        ij p;
+        load(g, x, p);
+        f(g, row_of(g), x, p);
       }
     }
   };
   int newest = INT32_MIN;
-  rows([&](int, bool in, float, int p) { if (in) newest = max(newest, p); });
+  lines([&](int, int row, const fj &, const ij &p) {
+    #pragma unroll
+    for (int j = 0; j < J; ++j) newest = row + j < R ? max(newest, p[j]) : newest;
+  });
   newest = wave_max(newest);
-  if (lane == 0) sm_a[wave] = newest;
+  if (lane == 0) sm_new[wave] = newest;
   bad = __syncthreads_or(bad);
-  if (speaker) {
+  if (h == 0 && layer == 0 && tid == 0) {              // one thread of the sequence
     const int now = bad ? len : min(R, budget);        // nothing changes for a sequence that is not sound
     if (a.kv_len_out) a.kv_len_out[b] = now; else a.new_len[b] = now;
     if (bad) atomicOr(a.dev_status, (unsigned)(R < 0 ? AMPH_DEV_KV_OVERFLOW : AMPH_DEV_BAD_PAGE));
   }
+  if (!bad && (a.weights_in != a.weights_out || a.pos_in != a.pos_out))               // elsewhere: all places first, then what moves
+    for (int i = tid; i < min(R, budget); i += NT) { w_out[i] = w[i]; pos_out[i] = pos[i]; }
   if (bad || R <= budget) {
     if (!a.fused && tid == 0) a.n_moves[unit] = 0;
-    if (!bad && !in_place) rows([&](int row, bool in, float x, int p) { if (in) { w_out[row] = x; pos_out[row] = p; } });
     return;
   }
   #pragma unroll
-  for (int i = 0; i < NW; ++i) newest = max(newest, sm_a[i]);
+  for (int i = 0; i < NW; ++i) newest = max(newest, sm_new[i]);
   const long long safe_from = (long long)newest - a.recent;           // positions above it are kept first
   auto key_of = [&](float x, int p) -> unsigned { return (long long)p > safe_from ? 0xffffffffu : rank_key(x); };
+  typedef unsigned uj __attribute__((ext_vector_type(J)));
+  uj kr[GROUPS];
+  auto line_keys = [&](int row, const fj &x, const ij &p, uj &k) {     // places behind the last row have the lowest key, as NaN has
+    #pragma unroll
+    for (int j = 0; j < J; ++j) k[j] = row + j < R ? key_of(x[j], p[j]) : 0u;
+  };
+  if constexpr (HELD) lines([&](int g, int row, const fj &x, const ij &p) { line_keys(row, x, p, kr[g]); });
+  auto keys = [&](auto f) {                            // f(g, first row, J keys)
+    if constexpr (HELD) {
+      #pragma unroll
+      for (int g = 0; g < GROUPS; ++g) if (g < live_groups) f(g, row_of(g), kr[g]);
+    } else {
+      lines([&](int g, int row, const fj &x, const ij &p) { uj k; line_keys(row, x, p, k); f(g, row, k); });
+    }
+  };
+  // sums over the waves before this one, and over all
+  auto before = [&](const int *sm, int &all) {
+    int s = 0;
+    all = 0;
+    #pragma unroll
+    for (int i = 0; i < NW; ++i) { const int v = sm[i]; s += i < wave ? v : 0; all += v; }
+    return s;
+  };
   int2 *moves = a.moves + (size_t)unit * a.most;
+  int2 *fused_moves = reinterpret_cast<int2 *>(sm_hole + (a.most + 1) / 2 * 2);      // (HELD)
   const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
 
   if (R == budget + 1) {
     // ---- the smallest key goes, the last row of that key
     unsigned least = 0xffffffffu;
-    rows([&](int, bool in, float x, int p) { if (in) least = min(least, key_of(x, p)); });
-    least = wave_fold(least, MinU());
-    if (lane == 0) sm_b[wave] = (int)least;
-    __syncthreads();
-    #pragma unroll
-    for (int i = 0; i < NW; ++i) least = min(least, (unsigned)sm_b[i]);
-    int gone = -1;
-    rows([&](int row, bool in, float x, int p) { if (in && key_of(x, p) == least) gone = max(gone, row); });
-    gone = wave_max(gone);
-    if (lane == 0) sm_c[wave] = gone;
-    __syncthreads();
-    #pragma unroll
-    for (int i = 0; i < NW; ++i) gone = max(gone, sm_c[i]);
-    rows([&](int row, bool in, float x, int p) {
-      if (in && row == budget && gone < budget) { w_out[gone] = x; pos_out[gone] = p; }
-      else if (in && !in_place && row < budget && row != gone) { w_out[row] = x; pos_out[row] = p; }
+    keys([&](int, int row, const uj &k) {
+      #pragma unroll
+      for (int j = 0; j < J; ++j) least = row + j < R ? min(least, k[j]) : least;
     });
+    least = wave_fold(least, MinU());
+    int gone = -1;                                     // the wave's: waves have their rows in order, so the last one of the least key counts
+    keys([&](int, int row, const uj &k) {
+      #pragma unroll
+      for (int j = 0; j < J; ++j) gone = row + j < R && k[j] == least ? row + j : gone;
+    });
+    gone = wave_max(gone);
+    if (lane == 0) { sm_b[wave] = (int)least; sm_c[wave] = gone; }
+    __syncthreads();
+    least = 0xffffffffu;
+    #pragma unroll
+    for (int i = 0; i < NW; ++i)
+      if (sm_c[i] >= 0 && (unsigned)sm_b[i] <= least) { least = (unsigned)sm_b[i]; gone = sm_c[i]; }
     const int2 one = make_int2(gone, budget);
+    if (tid == 0 && gone < budget) { w_out[gone] = w[budget]; pos_out[gone] = pos[budget]; }
     if (!a.fused) {
       if (tid == 0) { moves[0] = one; a.n_moves[unit] = gone < budget; }
     } else if (wave == 0 && gone < budget) {
@@ -743,33 +793,39 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     return;
   }
 
-  // ---- the smallest kept key among those that are no newest row's: `want` of the keys in [lo, hi] are kept
+  // ---- the smallest kept key: `want` of the keys in [lo, hi] are kept
   unsigned lo = 0xffffffffu, hi = 0u;
-  int safe = 0;
-  rows([&](int, bool in, float x, int p) {
-    const unsigned k = key_of(x, p);
-    const bool fixed = k == 0xffffffffu;
-    safe += __popcll(__ballot(in && fixed));
-    if (in && !fixed) { lo = min(lo, k); hi = max(hi, k); }
+  int count = 0;                                       // of rows of any key but the lowest; of newest rows in the upper half
+  keys([&](int, int, const uj &k) {
+    #pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const bool fixed = k[j] == 0xffffffffu;
+      count += (k[j] != 0u ? 1 : 0) + (fixed ? 0x10000 : 0);
+      lo = k[j] ? min(lo, k[j]) : lo;
+      hi = fixed ? hi : max(hi, k[j]);
+    }
   });
+  int some = count & 0xffff, safe = count >> 16;
+  some = wave_fold(some, AddI());
+  safe = wave_fold(safe, AddI());
   lo = wave_fold(lo, MinU());
   hi = wave_fold(hi, MaxU());
-  __syncthreads();                                     // (sm_a is read)
-  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; }
-  for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; sm_d[wave] = some; }
   __syncthreads();
-  safe = 0;
+  safe = some = 0;
   #pragma unroll
-  for (int i = 0; i < NW; ++i) { safe += sm_a[i]; lo = min(lo, (unsigned)sm_b[i]); hi = max(hi, (unsigned)sm_c[i]); }
-  int want = budget - safe, equal;
-  if (want <= 0) { lo = 0xffffffffu; want = budget; equal = safe; }
+  for (int i = 0; i < NW; ++i) { safe += sm_a[i]; some += sm_d[i]; lo = min(lo, (unsigned)sm_b[i]); hi = max(hi, (unsigned)sm_c[i]); }
+  int want = budget - safe;
+  bool all_equal = false;                              // all keys from lo on are kept
+  if (want <= 0) { lo = 0xffffffffu; want = budget; }
+  else if (some < budget) { lo = 0u; want = budget - some; }
   else {
     for (;;) {
       const unsigned span = hi - lo;
       const int shift = span >> 11 ? 21 - __clz(span) : 0;             // (bins: span >> shift < 2048)
-      rows([&](int, bool in, float x, int p) {
-        const unsigned k = key_of(x, p);
-        if (in && k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+      keys([&](int, int, const uj &k) {
+        #pragma unroll
+        for (int j = 0; j < J; ++j) if (k[j] - lo <= span) atomicAdd(&hist[(k[j] - lo) >> shift], 1);
       });
       __syncthreads();
       // from the top, thread t has PB bins; the bin at which the count reaches `want`
@@ -777,17 +833,13 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       int c[PB], mine = 0;
       #pragma unroll
       for (int i = 0; i < PB; ++i) { c[i] = hist[BINS - 1 - (tid * PB + i)]; mine += c[i]; }
-      int upto = mine;
-      #pragma unroll
-      for (int o = 1; o < WAVE; o <<= 1) {
-        const int v = __shfl_up(upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (lane == WAVE - 1) sm_a[wave] = upto;
+      int upto = wave_scan(mine);
+      if (lane == WAVE - 1) sm_e[wave] = upto;
       __syncthreads();
       #pragma unroll
       for (int i = 0; i < PB; ++i) hist[BINS - 1 - (tid * PB + i)] = 0;
-      for (int i = 0; i < wave; ++i) upto += sm_a[i];
+      int all;
+      upto += before(sm_e, all);
       int above = upto - mine;
       if (upto >= want && above < want) {
         #pragma unroll
@@ -800,91 +852,142 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       lo += (unsigned)sm_pick[0] << shift;
       hi = min(hi, lo + ((1u << shift) - 1));
       want = sm_pick[1];
-      equal = sm_pick[2];
-      if (shift == 0 || equal == want) break;          // one key; or all of the bin is kept
-    }
-  }
-  // kept: above hi; in [lo, hi] (one key, where not all are kept) the first `want`
-  const unsigned from_key = lo;
-  const bool all_equal = equal == want;
-  int eq = 0;
-  if (!all_equal) {
-    rows([&](int, bool in, float x, int p) { eq += __popcll(__ballot(in && key_of(x, p) == from_key)); });
-    if (lane == 0) sm_b[wave] = eq;
-    __syncthreads();
-    eq = 0;
-    for (int i = 0; i < wave; ++i) eq += sm_b[i];
-  }
-  const int eq_before = eq;
-  auto kept = [&](bool in, unsigned k) {
-    if (all_equal) return in && k >= from_key;
-    const uint64_t same = __ballot(in && k == from_key);
-    const bool keep = in && (k > from_key || (k == from_key && eq + lanes_before(same) < want));
-    eq += __popcll(same);
-    return keep;
-  };
-  int n_hole = 0, n_from = 0;
-  rows([&](int row, bool in, float x, int p) {
-    const bool keep = kept(in, key_of(x, p));
-    n_hole += __popcll(__ballot(in && !keep && row < budget));
-    n_from += __popcll(__ballot(keep && row >= budget));
-  });
-  __syncthreads();                                     // (sm_a is read)
-  if (lane == 0) { sm_a[wave] = n_hole; sm_c[wave] = n_from; }
-  __syncthreads();
-  int total = 0;
-  n_hole = n_from = 0;
-  for (int i = 0; i < NW; ++i) {
-    if (i < wave) { n_hole += sm_a[i]; n_from += sm_c[i]; }
-    total += sm_a[i];
-  }
-  eq = eq_before;
-  rows([&](int row, bool in, float x, int p) {
-    const bool keep = kept(in, key_of(x, p)), hole = in && !keep && row < budget;
-    const uint64_t mh = __ballot(hole);
-    if (hole) {
-      const int i = n_hole + lanes_before(mh);
-      if constexpr (HELD) sm_hole[i] = row; else moves[i].x = row;
-    }
-    n_hole += __popcll(mh);
-    if (keep && row < budget && !in_place) { w_out[row] = x; pos_out[row] = p; }
-  });
-  __syncthreads();
-  eq = eq_before;
-  rows([&](int row, bool in, float x, int p) {
-    const bool keep = kept(in, key_of(x, p)), mover = keep && row >= budget;
-    const uint64_t mf = __ballot(mover);
-    if (mover) {
-      const int i = n_from + lanes_before(mf);
-      if constexpr (HELD) {
-        const int d = sm_hole[i];
-        moves[i] = make_int2(d, row);
-        w_out[d] = x;
-        pos_out[d] = p;
-      } else {
-        moves[i].y = row;
+      const int in_bin = sm_pick[2];
+      all_equal = in_bin == want;
+      if (shift == 0 || all_equal) break;
+      if (in_bin <= FEW) {
+        // ---- few keys left: every wave ranks them all; the want-th largest, and how many are larger
+        const unsigned few_span = hi - lo;
+        keys([&](int, int, const uj &k) {
+          #pragma unroll
+          for (int j = 0; j < J; ++j) if (k[j] - lo <= few_span) sm_key[atomicAdd(&sm_few, 1)] = k[j];
+        });
+        __syncthreads();
+        const unsigned own = lane < in_bin ? sm_key[lane] : 0u;        // (in the order they came: only their values count)
+        int larger = 0, same = 0;
+        for (int s = 0; s < in_bin; ++s) {
+          const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)own, s);
+          larger += o > own ? 1 : 0;
+          same += o == own ? 1 : 0;
+        }
+        const uint64_t at_want = __ballot(lane < in_bin && larger < want && larger + same >= want);
+        const int l = __builtin_ctzll(at_want);
+        lo = (unsigned)__builtin_amdgcn_readlane((int)own, l);
+        want -= __builtin_amdgcn_readlane(larger, l);
+        all_equal = want == __builtin_amdgcn_readlane(same, l);
+        break;
       }
     }
-    n_from += __popcll(mf);
-  });
-  if constexpr (!HELD) {                               // (in place the weights change only when nobody reads them any more)
+  }
+  // ---- kept: all keys above lo, and of those that are lo the first `want`; then the places below the budget and the rows behind it
+  const unsigned from_key = lo;
+  int eq = 0;
+  if (!all_equal) {
+    keys([&](int, int row, const uj &k) {
+      #pragma unroll
+      for (int j = 0; j < J; ++j) eq += k[j] == from_key && row + j < R ? 1 : 0;
+    });
+    eq = wave_fold(eq, AddI());
+    if (lane == 0) sm_new[wave] = eq;                  // (what it held has been read by all since the barrier before)
     __syncthreads();
-    for (int i = tid; i < total; i += NT) {
-      const int2 mv = moves[i];
-      w_out[mv.x] = w[mv.y];
-      pos_out[mv.x] = pos[mv.y];
+    int all;
+    eq = before(sm_new, all);
+  }
+  const int eq_before = eq;
+  // the J rows that a lane keeps, as bits; all lanes, groups in order (eq: the equal keys before the group)
+  auto kept = [&](int row, const uj &k) {
+    unsigned keep = 0;
+    if (all_equal) {                                   // (lo is not the lowest key, which has no bin)
+      #pragma unroll
+      for (int j = 0; j < J; ++j) keep |= (k[j] >= from_key ? 1u : 0u) << j;
+    } else {
+      unsigned same = 0;
+      #pragma unroll
+      for (int j = 0; j < J; ++j) {
+        keep |= (k[j] > from_key ? 1u : 0u) << j;
+        same |= (k[j] == from_key && row + j < R ? 1u : 0u) << j;      // (the lowest key is also that of places that are no rows)
+      }
+      const int mine = __popc(same), upto = wave_scan(mine);
+      int left = want - eq - (upto - mine);            // of the lane's equal keys, so many are kept: its first
+      #pragma unroll
+      for (int j = 0; j < J; ++j) if (same >> j & 1u) { if (left > 0) keep |= 1u << j; --left; }
+      eq += __builtin_amdgcn_readlane(upto, WAVE - 1);
     }
+    return keep;
+  };
+  auto below = [&](int row) { return row >= budget ? 0u : budget - row >= J ? (1u << J) - 1 : (1u << (budget - row)) - 1; };
+  unsigned bits[GROUPS];                               // (HELD: found once)
+  int n_hole = 0, n_from = 0;
+  keys([&](int g, int row, const uj &k) {
+    const unsigned keep = kept(row, k), lt = below(row);
+    if constexpr (HELD) bits[g] = keep;
+    n_hole += __popc(~keep & lt);
+    n_from += __popc(keep & ~lt);
+  });
+  n_hole = wave_fold(n_hole, AddI());
+  n_from = wave_fold(n_from, AddI());
+  if (lane == 0) { sm_a[wave] = n_hole; sm_c[wave] = n_from; }         // (read by all: a barrier of the search or of the equal keys is behind)
+  __syncthreads();
+  int total;
+  n_hole = before(sm_a, total);
+  n_from = before(sm_c, total);
+  const int from0 = n_from;
+  auto listed = [&](auto f) {                          // f(bits of the lane's kept rows, its first row)
+    eq = eq_before;
+    if constexpr (HELD) {
+      #pragma unroll
+      for (int g = 0; g < GROUPS; ++g) if (g < live_groups) f(bits[g], row_of(g));
+    } else {
+      keys([&](int, int row, const uj &k) { f(kept(row, k), row); });
+    }
+  };
+  listed([&](unsigned keep, int row) {
+    unsigned m = ~keep & below(row);
+    const int mine = __popc(m), upto = wave_scan(mine);
+    for (int i = n_hole + upto - mine; m; m &= m - 1, ++i) {
+      const int r = row + __builtin_ctz(m);
+      if constexpr (HELD) sm_hole[i] = r; else moves[i].x = r;
+    }
+    n_hole += __builtin_amdgcn_readlane(upto, WAVE - 1);
+  });
+  __syncthreads();
+  n_from = from0;
+  listed([&](unsigned keep, int row) {
+    unsigned m = keep & ~below(row);
+    const int mine = __popc(m), upto = wave_scan(mine);
+    for (int i = n_from + upto - mine; m; m &= m - 1, ++i) {
+      const int r = row + __builtin_ctz(m);
+      if constexpr (HELD) {
+        const int2 mv = make_int2(sm_hole[i], r);
+        if (a.fused) fused_moves[i] = mv; else moves[i] = mv;
+      } else {
+        moves[i].y = r;
+      }
+    }
+    n_from += __builtin_amdgcn_readlane(upto, WAVE - 1);
+  });
+  __syncthreads();
+  for (int i = tid; i < total; i += NT) {              // (rows behind the budget, which nobody writes, to places below it)
+    int2 mv;
+    if constexpr (HELD) { if (a.fused) mv = fused_moves[i]; else mv = moves[i]; } else mv = moves[i];
+    w_out[mv.x] = w[mv.y];
+    pos_out[mv.x] = pos[mv.y];
   }
   if (!a.fused) {
     if (tid == 0) a.n_moves[unit] = total;
     return;
   }
-  __syncthreads();
-  for (int i0 = wave * 16; i0 < total; i0 += NW * 16) evict_move_rows<T, DH>(a.c, row_table, base, moves, i0, total);
+  for (int i0 = wave * 16; i0 < total; i0 += NW * 16) {
+    if constexpr (HELD) evict_move_rows<T, DH>(a.c, row_table, base, fused_moves, i0, total);
+    else evict_move_rows<T, DH>(a.c, row_table, base, moves, i0, total);
+  }
 }
 
 constexpr int EVICT_MOVES = 64;                        // moves of a workgroup: 16 a wave
 
+// Many moves.  Bound by HBM: a value row's dims lie 64 bytes apart, each among the same dim of its step's other rows, so the lines of every
+// step that a row leaves or enters are read whole.  8191 -> 2048 rows in 16 heads of 128 dims (1640 moves each, 27 MB of rows in some
+// 60 MB of lines): 16.3 us.  (Whole steps through LDS, where the rows change places: 16.8 and 18.0 us, a wave for all dims and for a quarter.)
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a, int32_t *kv_len_out) {
   const int tid = threadIdx.x, wave = tid >> 6, unit = blockIdx.x;
@@ -918,7 +1021,7 @@ static hipError_t paged_evict_shape(hipStream_t st, PagedEvictArgs a, int n_laye
   if (same_len) a.kv_len_out = nullptr;
   a.fused = a.most <= EVICT_FUSED;
   const int cap = a.seqs.cap;
-  const size_t lds = (size_t)a.most * 4;
+  const size_t lds = (size_t)a.most * (a.fused ? 12 : 4) + 8;
   #define EVICT(NT, RPT) hipLaunchKernelGGL((k_evict<T, DH, NT, RPT>), dim3(units), dim3(NT), RPT ? lds : 0, st, a)
   if (cap <= 512) EVICT(256, 2);
   else if (cap <= 2048) EVICT(256, 8);
@@ -926,9 +1029,10 @@ static hipError_t paged_evict_shape(hipStream_t st, PagedEvictArgs a, int n_laye
   else if (cap <= 16384) EVICT(1024, 16);
   else EVICT(1024, 0);
   #undef EVICT
-  if (!a.fused || same_len)
-    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(units, a.fused ? 1 : std::min((a.most + EVICT_MOVES - 1) / EVICT_MOVES, 65535)), dim3(256), 0, st, a,
-                       len_out);
+  if (!a.fused)
+    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(units, std::min((a.most + EVICT_MOVES - 1) / EVICT_MOVES, 65535)), dim3(256), 0, st, a, len_out);
+  else if (same_len)
+    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(a.seqs.n_seq * a.c.n_kv), dim3(256), 0, st, a, len_out);
   return hipGetLastError();
 }
 

@@ -447,6 +447,17 @@ def test_evict_equal_and_special_weights(weights, positions):
 def test_evict_long():
     evict_case("bf16", 1, 64, [20011], 5000, 1000, layers=1, page=256)
     evict_case("bf16", 1, 64, [9000, 40], 8999, 1, layers=1, page=128, weights="ties")
+    evict_case("f32", 1, 64, [17000, 300], 400, 0, layers=1, page=256, in_place=True, weights="ties")
+    evict_case("bf16", 1, 64, [16999], 16999, 3, layers=1, page=1024, in_place=True)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("L,budget,per", [(700, 333, 11), (1999, 1000, None), (1999, 700, 100), (5000, 1111, None), (12000, 2900, None)])
+def test_evict_many_moves(dtype, dim, L, budget, per):
+    """More than the choosing workgroup moves itself: by key steps below the budget, the last of them cut by it; one sequence drops a single
+    row, one none."""
+    evict_case(dtype, 1, dim, [L, budget, budget // 2], budget, budget // 3, page=64, per=per, layers=1, in_place=True)
+    evict_case(dtype, 2, dim, [L], budget, 0, page=64, per=per, layers=1, weights="ties", positions="mixed")
 
 
 def test_evict_new_rows_and_tables():

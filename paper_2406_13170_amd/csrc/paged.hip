@@ -496,11 +496,25 @@ template hipError_t launch_paged_attn<bf16_t>(hipStream_t, const PagedAttnArgs &
 // and sines into LDS, then a wave takes head after head.  A whole step of values is turned round in registers, so that its
 // lines are written whole; of a part of one every element is written on its own.
 // =====================================================================================================
+// Sine and cosine of an angle in turns: the nearest quarter turn is taken off in 64 bits, what is left, up to half a quarter, goes through
+// the Taylor polynomials (their next terms are 2e-9 and 2.5e-8 there), and the quarters swap and negate the two.
+__device__ __forceinline__ void sincos_turns(double turns, float *sn, float *cs) {
+  const double quarters = turns * 4.0, n = rint(quarters);
+  const float x = (float)(quarters - n) * 1.57079632679f, x2 = x * x;
+  const float s = x + x * x2 * (-1.0f / 6 + x2 * (1.0f / 120 + x2 * (-1.0f / 5040 + x2 * (1.0f / 362880))));
+  const float c = 1.0f + x2 * (-0.5f + x2 * (1.0f / 24 + x2 * (-1.0f / 720 + x2 * (1.0f / 40320))));
+  const int q = (int)(n - 4.0 * floor(n * 0.25));
+  const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+  *sn = q & 2 ? -a : a;
+  *cs = (q + 1) & 2 ? -b : b;
+}
+template <int N> struct Rows { static constexpr int value = N; };
+
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, const PagedRope rope) {
   constexpr int PER = Elem<T>::PER, KSTEP = 4 * PER, HALF = DH / 2, LPR = HALF / PER, RPP = WAVE / LPR;   // LPR lanes: a row's pairs
   typedef T frag __attribute__((ext_vector_type(PER)));
-  __shared__ float2 sm_cs[KSTEP][HALF + 1];
+  __shared__ __align__(16) float sm_c[KSTEP][HALF + 4], sm_s[KSTEP][HALF + 4];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, b = blockIdx.y;
   const int len = a.seqs.kv_len[b], fresh = a.seqs.n_valid ? paged_new(a.seqs.n_new, a.seqs.n_valid[b]) : a.seqs.n_new;
   const int L = paged_rows(len, fresh, a.seqs.cap);
@@ -521,10 +535,10 @@ __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, c
   for (int t = tid; t < live * HALF; t += 256) {
     const int r = t / HALF, i = t % HALF;
     // turns, in 64 bits: of a far position's angle 32 bits would leave a few places; then what is left of the last whole turn
-    const double turns = (double)(a.pos ? a.pos[new0 + r] : row0 + r) * rope.turns[i];
     float sn, cs;
-    sincosf((float)((turns - rint(turns)) * 6.283185307179586), &sn, &cs);
-    sm_cs[r][i] = make_float2(cs, sn);
+    sincos_turns((double)(a.pos ? a.pos[new0 + r] : row0 + r) * rope.turns[i], &sn, &cs);
+    sm_c[r][i] = cs;
+    sm_s[r][i] = sn;
   }
   __syncthreads();
   const size_t page = (size_t)id * a.c.page_stride + (size_t)(step - pg * psteps) * (KSTEP * DH);
@@ -536,25 +550,36 @@ __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, c
       const T *src = (const T *)(is_q ? a.q : a.k) + new0 * (is_q ? a.ld_q : a.ld_k) + (size_t)h * DH;
       const size_t ld = is_q ? a.ld_q : a.ld_k;
       T *dst = is_q ? (T *)a.q_out + (new0 * a.n_heads + h) * DH : (T *)a.c.k + page + (size_t)h * a.c.head_stride;
-      const int p = (lane % LPR) * PER;
-      for (int r = lane / LPR; r < live; r += RPP) {
-        const frag lo = *reinterpret_cast<const frag *>(src + r * ld + p), hi = *reinterpret_cast<const frag *>(src + r * ld + HALF + p);
-        frag x, y;
+      const int p = (lane % LPR) * PER, r0 = lane / LPR;
+      auto pass = [&](auto tag) {                      // N x RPP rows, all asked for before the first is used; past the last one: that again
+        constexpr int N = decltype(tag)::value;
+        frag lo[N], hi[N];
         #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-          const float2 cs = sm_cs[r][p + e];
-          const float u = Elem<T>::to_f32(lo[e]), v = Elem<T>::to_f32(hi[e]);
-          x[e] = Elem<T>::from_f32(u * cs.x - v * cs.y);
-          y[e] = Elem<T>::from_f32(v * cs.x + u * cs.y);
+        for (int i = 0; i < N; ++i) {
+          const T *at = src + (size_t)min(r0 + i * RPP, live - 1) * ld + p;
+          lo[i] = __builtin_nontemporal_load(reinterpret_cast<const frag *>(at));
+          hi[i] = __builtin_nontemporal_load(reinterpret_cast<const frag *>(at + HALF));
         }
-        if (is_q) {
-          *reinterpret_cast<frag *>(dst + (size_t)r * a.n_heads * DH + p) = x;
-          *reinterpret_cast<frag *>(dst + (size_t)r * a.n_heads * DH + HALF + p) = y;
-        } else {
-          *reinterpret_cast<frag *>(dst + k_tiled_index<T>(k0 + r, p, DH)) = x;
-          *reinterpret_cast<frag *>(dst + k_tiled_index<T>(k0 + r, HALF + p, DH)) = y;
+        #pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = r0 + i * RPP;
+          if (r >= live) continue;
+          float cs[PER], sn[PER];
+          #pragma unroll
+          for (int e = 0; e < PER; e += 4) { load4<float>(&sm_c[r][p + e], cs + e); load4<float>(&sm_s[r][p + e], sn + e); }
+          frag x, y;
+          #pragma unroll
+          for (int e = 0; e < PER; ++e) {
+            const float u = Elem<T>::to_f32(lo[i][e]), v = Elem<T>::to_f32(hi[i][e]);
+            x[e] = Elem<T>::from_f32(u * cs[e] - v * sn[e]);
+            y[e] = Elem<T>::from_f32(v * cs[e] + u * sn[e]);
+          }
+          T *to = is_q ? dst + (size_t)r * a.n_heads * DH : dst;
+          *reinterpret_cast<frag *>(to + (is_q ? p : (int)k_tiled_index<T>(k0 + r, p, DH))) = x;
+          *reinterpret_cast<frag *>(to + (is_q ? HALF + p : (int)k_tiled_index<T>(k0 + r, HALF + p, DH))) = y;
         }
-      }
+      };
+      if (live <= RPP) pass(Rows<1>{}); else pass(Rows<KSTEP / RPP>{});
       if (!is_q && lane < live) {
         const size_t at = ((size_t)b * a.c.n_kv + h) * a.c.table_pages * a.c.page_rows + row0 + lane;
         if (a.weights) a.weights[at] = 0.f;
@@ -569,7 +594,7 @@ __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, c
         const int li = lane % LPV, grp = lane / LPV;
         frag x[UN];
         #pragma unroll
-        for (int j = 0; j < UN; ++j) x[j] = *reinterpret_cast<const frag *>(src + (size_t)(grp * UN + j) * a.ld_v + li * PER);
+        for (int j = 0; j < UN; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const frag *>(src + (size_t)(grp * UN + j) * a.ld_v + li * PER));
         #pragma unroll
         for (int e = 0; e < PER; ++e) {
           run y;
@@ -590,9 +615,10 @@ template <typename T>
 hipError_t launch_paged_append(hipStream_t st, const PagedAppendArgs &a, const PagedRope &rope, int d_h) {
   constexpr int KSTEP = 4 * Elem<T>::PER;
   const int steps = (a.seqs.n_new + KSTEP - 2) / KSTEP + 1, units = (a.q ? a.n_heads : 0) + 2 * a.c.n_kv;
-  // heads are spread over workgroups until there are two for every compute unit
+  // Heads are spread over workgroups until there are four for every compute unit, as many heads for every wave (four prompts of 256 to
+  // 1024 rows, 32 heads of 128 dims and as many key heads, us: one to a wave 30.6, two 28.9 and 34.0, three 27.5, six 34.3).
   const long long have = (long long)steps * a.seqs.n_seq;
-  const int z = (int)std::min<long long>((units + 3) / 4, std::max<long long>(1, (512 + have - 1) / have));
+  const int m = (int)std::max<long long>(1, std::min<long long>(units, units * have / 4096)), z = (units + 4 * m - 1) / (4 * m);
   const dim3 grid(steps, a.seqs.n_seq, z);
   if (d_h == 128) hipLaunchKernelGGL((k_paged_append<T, 128>), grid, dim3(256), 0, st, a, rope);
   else hipLaunchKernelGGL((k_paged_append<T, 64>), grid, dim3(256), 0, st, a, rope);

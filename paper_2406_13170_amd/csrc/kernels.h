@@ -199,7 +199,7 @@ struct PagedSeqs {            // rows of sequence b: kv_len[b], then n_valid[b] 
 struct PagedAttnArgs {
   PagedPages c; PagedSeqs seqs;
   const void *q; size_t ld_q; void *out;
-  int n_heads;
+  int n_heads, group, n_qg, walks;                                // filled in by the launch: query heads a key head, their groups, walks a sequence
   const float *weights_in; float *weights_out;
   uint32_t *dev_status;
   int32_t *plan; float2 *stats; float *partials, *scores;        // in the workspace: paged_attn_ws_bytes

@@ -17,6 +17,17 @@ __device__ __forceinline__ uint4 ldb16_stream(__amdgpu_buffer_rsrc_t r, int at) 
 }
 constexpr float PAGED_LOWEST = -3.402823466e38f;       // of a running maximum: no finite score is below it, and -inf - it is -inf
 
+// Inclusive sum over the lanes of a wave, inside the vector ALU: shifts within rows of 16, then the rows' last lanes passed on.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
+  return v;
+}
+
 __device__ __forceinline__ int paged_len(const PagedSeqs &s, int b) {
   return paged_rows(s.kv_len[b], s.n_valid ? paged_new(s.n_new, s.n_valid[b]) : s.n_new, s.cap);
 }
@@ -39,6 +50,8 @@ struct PA {
   static constexpr int PART = NQ * DH + 2 * NQ;    // floats of one partial: O, then m, then l (-1: a bad page)
 };
 
+template <int N> struct Rows { static constexpr int value = N; };
+
 // ALONE: a workgroup for every walk (one key head's query group of one sequence).  Otherwise the walks' key steps are dealt out
 // in equal pieces (paged_plan.h) and k_paged_fold joins what was cut.
 template <typename T, int DH, int NQB, bool ALONE>
@@ -50,7 +63,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
   __shared__ int sm_len[ALONE ? 1 : PAGED_MAX_SEQ], sm_sum[PAGED_WAVES], sm_at[2];
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r16 = lane & 15;
-  const int n_seq = a.seqs.n_seq, G = a.n_heads / a.c.n_kv, n_qg = (G + NQ - 1) / NQ, U = a.c.n_kv * n_qg;
+  const int n_seq = a.seqs.n_seq, G = a.group, n_qg = a.n_qg, U = a.walks;
   const int psteps = a.c.page_rows / KSTEP;            // key steps of a page
   const float scale = 1.4426950408889634f * rsqrtf((float)DH);
   const float NEG_INF = -__builtin_huge_valf();
@@ -125,20 +138,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
           for (int c = 0; c < 4; ++c) sv[qb][t * 4 + c] = acc[c] * scale;
         }
     };
-    // the running maximum, and the step's probabilities in the place of its scores
-    auto softmax = [&](int i, float (&sv)[NQB][PER]) {
+    // the running maximum, and the step's probabilities
+    auto softmax = [&](int i, float (&sv)[NQB][PER], float (&pv)[NQB][PER]) {
       const int key0 = (s + wave + PAGED_WAVES * i) * KSTEP;
       #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
         if (key0 + KSTEP > L) {
           #pragma unroll
           for (int j = 0; j < PER; ++j) if (key0 + g * PER + j >= L) sv[qb][j] = NEG_INF;
-        }
-        if (score && qb * 16 + r16 < live_q) {         // (cap is a multiple of the step: rows behind the last have their place)
-          float *to = score + (size_t)(qb * 16 + r16) * a.seqs.cap + key0 + g * PER;
-          #pragma unroll
-          for (int j = 0; j < PER; j += 4)
-            *reinterpret_cast<float4 *>(to + j) = make_float4(sv[qb][j], sv[qb][j + 1], sv[qb][j + 2], sv[qb][j + 3]);
         }
         float mx = sv[qb][0], ls = 0.f;
         #pragma unroll
@@ -152,8 +159,19 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
           m_run[qb] = mn;
         }
         #pragma unroll
-        for (int j = 0; j < PER; ++j) { sv[qb][j] = paged_exp2(sv[qb][j] - mn); ls += sv[qb][j]; }
+        for (int j = 0; j < PER; ++j) { pv[qb][j] = paged_exp2(sv[qb][j] - mn); ls += pv[qb][j]; }
         l_run[qb] += ls;
+      }
+    };
+    // for the weights (cap is a multiple of the step: rows behind the last have their place)
+    auto keep_scores = [&](int i, const float (&sv)[NQB][PER]) {
+      #pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) {
+        if (qb * 16 + r16 >= live_q) continue;
+        float *to = score + (size_t)(qb * 16 + r16) * a.seqs.cap + (s + wave + PAGED_WAVES * i) * KSTEP + g * PER;
+        #pragma unroll
+        for (int j = 0; j < PER; j += 4)
+          *reinterpret_cast<float4 *>(to + j) = make_float4(sv[qb][j], sv[qb][j + 1], sv[qb][j + 2], sv[qb][j + 3]);
       }
     };
     auto values = [&](int i, const float (&pv)[NQB][PER]) {
@@ -196,12 +214,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
         const bool more = i + 1 < n_w;
         if (more && ((i + 1) & 63) == 0) look_up(i + 1);
         at = step_base(i + 1);
-        float sv[NQB][PER];
+        float sv[NQB][PER], pv[NQB][PER];
         scores(i, sv);
         load_k(at, more);
-        softmax(i, sv);
-        values(i, sv);
+        softmax(i, sv, pv);
+        values(i, pv);
         load_v(at, more);
+        if (score) keep_scores(i, sv);                 // (behind the loads, which would otherwise wait for the stores)
       }
     }
     const bool wave_bad = __any(bad);
@@ -211,9 +230,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       const float l = lanes_xor32(lanes_xor16(l_run[qb], AddF()), AddF());
-      if (g == 0) { sm_m[wave][qb * 16 + r16] = m_run[qb]; sm_l[wave][qb * 16 + r16] = wave_bad ? -1.f : l; }
-      #pragma unroll
-      for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sm_o[wave][qb * 16 + r16][db * 16 + g * 4]) = O[qb][db];
+      if (qb * 16 + r16 < live_q) {
+        if (g == 0) { sm_m[wave][qb * 16 + r16] = m_run[qb]; sm_l[wave][qb * 16 + r16] = wave_bad ? -1.f : l; }
+        #pragma unroll
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sm_o[wave][qb * 16 + r16][db * 16 + g * 4]) = O[qb][db];
+      }
     }
     __syncthreads();
     const bool any_bad = sm_l[0][0] < 0.f || sm_l[1][0] < 0.f || sm_l[2][0] < 0.f || sm_l[3][0] < 0.f;
@@ -255,59 +276,59 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     return;
   }
 
-  // ---- the sequences' lengths and the steps before each, thread t for sequences 4 t .. 4 t + 3
-  constexpr int PT = PAGED_MAX_SEQ / 256;
-  int st[PT], sum = 0;
-  bool over = false;
-  #pragma unroll
-  for (int i = 0; i < PT; ++i) {
-    const int b = tid * PT + i;
-    int L = 0;
-    if (b < n_seq) {
-      L = paged_len(a.seqs, b);
-      sm_len[b] = L;
-      over |= L < 0;
+  // ---- the sequences' lengths and the steps before each, thread t for sequences PT t .. PT t + PT - 1
+  int all = 0, chunk = 0;
+  long long first = 0;
+  auto deal = [&](auto tag) {
+    constexpr int PT = decltype(tag)::value;
+    int st[PT], sum = 0;
+    bool over = false;
+    #pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int b = tid * PT + i;
+      int L = 0;
+      if (b < n_seq) {
+        L = paged_len(a.seqs, b);
+        sm_len[b] = L;
+        over |= L < 0;
+      }
+      st[i] = L > 0 ? (L + KSTEP - 1) / KSTEP : 0;
+      sum += st[i];
     }
-    st[i] = L > 0 ? (L + KSTEP - 1) / KSTEP : 0;
-    sum += st[i];
-  }
-  int upto = sum;
-  #pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) {
-    const int v = __shfl_up(upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == WAVE - 1) sm_sum[wave] = upto;
-  if (blockIdx.x == 0 && over) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
-  __syncthreads();
-  int before = upto - sum, all = 0;
-  #pragma unroll
-  for (int w = 0; w < PAGED_WAVES; ++w) { before += w < wave ? sm_sum[w] : 0; all += sm_sum[w]; }
+    const int upto = wave_scan(sum);
+    if (lane == WAVE - 1) sm_sum[wave] = upto;
+    if (blockIdx.x == 0 && over) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
+    __syncthreads();
+    int before = upto - sum;
+    #pragma unroll
+    for (int w = 0; w < PAGED_WAVES; ++w) { before += w < wave ? sm_sum[w] : 0; all += sm_sum[w]; }
+    chunk = paged_chunk((long long)all * U, PAGED_WGS);
+    first = (long long)blockIdx.x * chunk;
+    #pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int b = tid * PT + i;
+      if (b < n_seq) {
+        if (blockIdx.x == 0) { a.plan[b] = before; a.plan[n_seq + 1 + b] = sm_len[b]; }
+        const long long off = first - (long long)before * U;
+        if (off >= 0 && off < (long long)st[i] * U) { sm_at[0] = b; sm_at[1] = (int)off; }
+      }
+      before += st[i];
+    }
+  };
+  if (n_seq <= 256) deal(Rows<1>{}); else deal(Rows<PAGED_MAX_SEQ / 256>{});
   const long long total = (long long)all * U;
-  const int chunk = paged_chunk(total, gridDim.x);
-  const long long first = (long long)blockIdx.x * chunk;
-  #pragma unroll
-  for (int i = 0; i < PT; ++i) {
-    const int b = tid * PT + i;
-    if (b < n_seq) {
-      if (blockIdx.x == 0) { a.plan[b] = before; a.plan[n_seq + 1 + b] = sm_len[b]; }
-      const long long off = first - (long long)before * U;
-      if (off >= 0 && off < (long long)st[i] * U) { sm_at[0] = b; sm_at[1] = (int)off; }
-    }
-    before += st[i];
-  }
   if (blockIdx.x == 0 && tid == 0) a.plan[n_seq] = all;
   if (first >= total) return;                          // (whole workgroup)
   __syncthreads();
-  int b = sm_at[0], u, s, left = (int)min((long long)chunk, total - first);
+  int b = __builtin_amdgcn_readfirstlane(sm_at[0]), u, s, left = __builtin_amdgcn_readfirstlane((int)min((long long)chunk, total - first));
   bool head_of_piece = true;
   {
-    const int steps = (sm_len[b] + KSTEP - 1) / KSTEP;
-    u = sm_at[1] / steps;
-    s = sm_at[1] - u * steps;
+    const int steps = (__builtin_amdgcn_readfirstlane(sm_len[b]) + KSTEP - 1) / KSTEP, at = __builtin_amdgcn_readfirstlane(sm_at[1]);
+    u = at / steps;
+    s = at - u * steps;
   }
   while (left > 0) {
-    const int L = sm_len[b], steps = (L + KSTEP - 1) / KSTEP, n = min(steps - s, left);
+    const int L = __builtin_amdgcn_readfirstlane(sm_len[b]), steps = (L + KSTEP - 1) / KSTEP, n = min(steps - s, left);
     walk(b, u, L, s, n, n == steps, 2 * blockIdx.x + (head_of_piece ? 0 : 1));
     head_of_piece = false;
     left -= n;
@@ -325,14 +346,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
 constexpr int PAGED_WROWS = 1024;
 
 template <typename T, int DH, int NQB>
-__global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, int wgs, int row_wgs) {
+__global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool alone, int row_wgs) {
   using C = PA<T, DH, NQB>;
   constexpr int KSTEP = C::KSTEP, NQ = C::NQ, LPQ = DH / 4, NG = 256 / LPQ;
   __shared__ __align__(16) float sm_o[NG][DH];
   __shared__ float sm_m[NG], sm_l[NG];
   __shared__ float2 sm_ml[32];
-  const int tid = threadIdx.x, n_seq = a.seqs.n_seq, G = a.n_heads / a.c.n_kv, n_qg = (G + NQ - 1) / NQ, U = a.c.n_kv * n_qg;
-  const bool alone = wgs == 0;
+  const int tid = threadIdx.x, n_seq = a.seqs.n_seq, G = a.group, n_qg = a.n_qg, U = a.walks;
   const int outs = alone ? 0 : n_seq * a.n_heads;
   const int item = (int)blockIdx.x - outs;
   const int bh = item < 0 ? blockIdx.x : item / row_wgs;                       // (sequence, head) or (sequence, key head)
@@ -341,7 +361,7 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, int w
   if (L < 0) return;
   const int steps = (L + KSTEP - 1) / KSTEP;
   const int pre = alone ? 0 : a.plan[b];
-  const int chunk = alone ? 1 : paged_chunk((long long)a.plan[n_seq] * U, wgs);
+  const int chunk = alone ? 1 : paged_chunk((long long)a.plan[n_seq] * U, PAGED_WGS);
 
   if (item < 0) {
     const int head = bh % a.n_heads, h = head / G, q = head % G, d4 = (tid % LPQ) * 4, grp = tid / LPQ;
@@ -465,9 +485,12 @@ size_t paged_attn_ws_bytes(int n_seq, int n_heads, int n_kv, int d_h, int cap, b
 }
 
 template <typename T, int DH, int NQB>
-static hipError_t paged_attn_shape(hipStream_t st, const PagedAttnArgs &a) {
+static hipError_t paged_attn_shape(hipStream_t st, PagedAttnArgs a) {
   using C = PA<T, DH, NQB>;
-  const int G = a.n_heads / a.c.n_kv, walks = a.seqs.n_seq * a.c.n_kv * ((G + C::NQ - 1) / C::NQ);
+  a.group = a.n_heads / a.c.n_kv;
+  a.n_qg = (a.group + C::NQ - 1) / C::NQ;
+  a.walks = a.c.n_kv * a.n_qg;
+  const int walks = a.seqs.n_seq * a.walks;
   const bool alone = paged_alone(a, C::KSTEP), weights = a.weights_out != nullptr;
   if (alone)
     hipLaunchKernelGGL((k_paged_attn<T, DH, NQB, true>), dim3(walks), dim3(256), 0, st, a);
@@ -477,7 +500,7 @@ static hipError_t paged_attn_shape(hipStream_t st, const PagedAttnArgs &a) {
   const long long grid = (alone ? 0ll : (long long)a.seqs.n_seq * a.n_heads) + (long long)a.seqs.n_seq * a.c.n_kv * row_wgs;
   if (grid > 0x7fffffffll) return hipErrorInvalidValue;
   if (grid)
-    hipLaunchKernelGGL((k_paged_fold<T, DH, NQB>), dim3((unsigned)grid), dim3(256), 0, st, a, alone ? 0 : PAGED_WGS, std::max(row_wgs, 1));
+    hipLaunchKernelGGL((k_paged_fold<T, DH, NQB>), dim3((unsigned)grid), dim3(256), 0, st, a, alone, std::max(row_wgs, 1));
   return hipGetLastError();
 }
 
@@ -508,8 +531,6 @@ __device__ __forceinline__ void sincos_turns(double turns, float *sn, float *cs)
   *sn = q & 2 ? -a : a;
   *cs = (q + 1) & 2 ? -b : b;
 }
-template <int N> struct Rows { static constexpr int value = N; };
-
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, const PagedRope rope) {
   constexpr int PER = Elem<T>::PER, KSTEP = 4 * PER, HALF = DH / 2, LPR = HALF / PER, RPP = WAVE / LPR;   // LPR lanes: a row's pairs
@@ -673,17 +694,6 @@ __device__ __forceinline__ void evict_move_rows(const PagedPages &c, const int32
     #pragma unroll
     for (int p = 0; p < SEGS; ++p) stg16(K + dpage + k_tiled_index<T>(dr, p * PIECE + sub * (PIECE / 4), DH), k[p]);
   }
-}
-
-// Inclusive sum over the lanes of a wave, inside the vector ALU: shifts within rows of 16, then the rows' last lanes passed on.
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
-  return v;
 }
 
 // NT threads.  Rows are dealt in order to waves, groups, lanes, J to a lane; RPT > 0: a lane keeps the keys of its RPT rows in registers

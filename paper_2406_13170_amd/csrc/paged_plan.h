@@ -31,8 +31,14 @@ struct PagedWalk {
 };
 __host__ __device__ inline PagedWalk paged_walk(long long first, int steps, int chunk) {
   PagedWalk p;
-  p.w0 = (int)(first / chunk);
-  p.w1 = (int)((first + steps - 1) / chunk);
+  const unsigned long long last = (unsigned long long)first + steps - 1;
+  if (last >> 32) {                           // (a 64-bit division costs some hundred instructions)
+    p.w0 = (int)(first / chunk);
+    p.w1 = (int)(last / chunk);
+  } else {
+    p.w0 = (int)((unsigned)first / (unsigned)chunk);
+    p.w1 = (int)((unsigned)last / (unsigned)chunk);
+  }
   p.begins = first == (long long)p.w0 * chunk;
   return p;
 }

@@ -787,6 +787,7 @@ const char *paged_kv_fault(const amph_config &c, const amph_paged_kv *kv, int n_
   if (kv->page_stride > far / kv->n_pages || kv->head_stride > far / kv->n_kv_heads || kv->layer_stride > far / std::max(n_layers, 1))
     return "strides too large";
   if ((int64_t)std::max(n_layers, 1) * kv->n_seq * kv->n_kv_heads > (1 << 30)) return "too many layers";
+  if ((int64_t)kv->n_seq * c.n_heads * kv->max_pages * kv->page_rows > (int64_t)1 << 40) return "too many rows in all";
   return nullptr;
 }
 }  // namespace amph

@@ -277,8 +277,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
   }
 
   // ---- the sequences' lengths and the steps before each, thread t for sequences PT t .. PT t + PT - 1
-  int all = 0, chunk = 0;
-  long long first = 0;
+  int all = 0;
+  long long first = 0, last = 0;
   auto deal = [&](auto tag) {
     constexpr int PT = decltype(tag)::value;
     int st[PT], sum = 0;
@@ -302,8 +302,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     int before = upto - sum;
     #pragma unroll
     for (int w = 0; w < PAGED_WAVES; ++w) { before += w < wave ? sm_sum[w] : 0; all += sm_sum[w]; }
-    chunk = paged_chunk((long long)all * U, PAGED_WGS);
-    first = (long long)blockIdx.x * chunk;
+    const PagedDeal pieces = paged_deal((long long)all * U);
+    first = pieces.begin(blockIdx.x);
+    last = pieces.begin(blockIdx.x + 1);
     #pragma unroll
     for (int i = 0; i < PT; ++i) {
       const int b = tid * PT + i;
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
   if (blockIdx.x == 0 && tid == 0) a.plan[n_seq] = all;
   if (first >= total) return;                          // (whole workgroup)
   __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(sm_at[0]), u, s, left = __builtin_amdgcn_readfirstlane((int)min((long long)chunk, total - first));
+  int b = __builtin_amdgcn_readfirstlane(sm_at[0]), u, s, left = __builtin_amdgcn_readfirstlane((int)(min(last, total) - first));
   bool head_of_piece = true;
   {
     const int steps = (__builtin_amdgcn_readfirstlane(sm_len[b]) + KSTEP - 1) / KSTEP, at = __builtin_amdgcn_readfirstlane(sm_at[1]);
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
   constexpr int KSTEP = C::KSTEP, NQ = C::NQ, LPQ = DH / 4, NG = 256 / LPQ;
   __shared__ __align__(16) float sm_o[NG][DH];
   __shared__ float sm_m[NG], sm_l[NG];
-  __shared__ float2 sm_ml[32];
+  __shared__ float2 sm_ml[8];
   const int tid = threadIdx.x, n_seq = a.seqs.n_seq, G = a.group, n_qg = a.n_qg, U = a.walks;
   const int outs = alone ? 0 : n_seq * a.n_heads;
   const int item = (int)blockIdx.x - outs;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
   if (L < 0) return;
   const int steps = (L + KSTEP - 1) / KSTEP;
   const int pre = alone ? 0 : a.plan[b];
-  const int chunk = alone ? 1 : paged_chunk((long long)a.plan[n_seq] * U, PAGED_WGS);
+  const PagedDeal pieces = alone ? PagedDeal{1, 0} : paged_deal((long long)a.plan[n_seq] * U);
 
   if (item < 0) {
     const int head = bh % a.n_heads, h = head / G, q = head % G, d4 = (tid % LPQ) * 4, grp = tid / LPQ;
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
       if (grp == 0) store4<T>(dst, z);
       return;
     }
-    const PagedWalk wk = paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, chunk);
+    const PagedWalk wk = paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, pieces);
     if (wk.w0 == wk.w1) return;                        // one workgroup had the whole walk and wrote its output
     const int np = wk.w1 - wk.w0 + 1, qi = q % NQ;
     // the chain of round trips is what this costs: four pieces a thread are asked for at once
@@ -424,17 +425,22 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
   if (row0 >= L) return;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
   bool bad = false;
-  for (int qa = 0; qa < G; qa += 32) {                 // 32 queries' maxima and sums at a time, eight lanes for each
-    const int q = qa + tid / 8, t8 = tid & 7;
+  constexpr int QB = 8;                                // queries at a time: their scores are asked for, then 32 lanes find each one's sum
+  for (int qa = 0; qa < G; qa += QB) {
+    const float *sc = a.scores + ((size_t)b * a.n_heads + (size_t)h * G + qa) * a.seqs.cap + min(row, a.seqs.cap - 4);
+    float4 v[QB];
+    #pragma unroll
+    for (int i = 0; i < QB; ++i) v[i] = *reinterpret_cast<const float4 *>(sc + (size_t)min(i, G - 1 - qa) * a.seqs.cap);
+    const int q = qa + tid / 32, t32 = tid & 31;
     float m = PAGED_LOWEST, l = 0.f;
     if (q < G) {
       const PagedWalk wk = alone ? PagedWalk{0, 0, true}
-                                 : paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, chunk);
+                                 : paged_walk((long long)pre * U + (long long)(h * n_qg + q / NQ) * steps, steps, pieces);
       if (wk.w0 == wk.w1) {
         const float2 st = a.stats[(size_t)b * a.n_heads + h * G + q];
-        if (t8 == 0) { m = st.x; l = st.y; bad |= l < 0.f; }
+        if (t32 == 0) { m = st.x; l = st.y; bad |= l < 0.f; }
       } else {
-        for (int i = t8; i <= wk.w1 - wk.w0; i += 8) {
+        for (int i = t32; i <= wk.w1 - wk.w0; i += 32) {
           const float *p = a.partials + (size_t)wk.place(wk.w0 + i) * C::PART + NQ * DH + q % NQ;
           const float mi = p[0], li = p[NQ], mn = fmaxf(m, mi);
           bad |= li < 0.f;
@@ -444,22 +450,20 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
       }
     }
     #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
+    for (int o = 1; o < 32; o <<= 1) {
       const float mo = __shfl_xor(m, o), lo = __shfl_xor(l, o), mn = fmaxf(m, mo);
       l = l * paged_exp2(m - mn) + lo * paged_exp2(mo - mn);
       m = mn;
     }
     __syncthreads();
-    if (t8 == 0) sm_ml[tid / 8] = make_float2(m, l > 0.f || l != l ? 1.0f / l : 0.f);
+    if (t32 == 0) sm_ml[tid / 32] = make_float2(m, l > 0.f || l != l ? 1.0f / l : 0.f);
     if (__syncthreads_or(bad)) return;
-    if (row < L) {
-      const float *sc = a.scores + ((size_t)b * a.n_heads + (size_t)h * G + qa) * a.seqs.cap + row;
-      for (int i = 0; i < min(32, G - qa); ++i) {
-        const float4 v = *reinterpret_cast<const float4 *>(sc + (size_t)i * a.seqs.cap);
-        const float2 ml = sm_ml[i];
-        acc[0] += paged_exp2(v.x - ml.x) * ml.y; acc[1] += paged_exp2(v.y - ml.x) * ml.y;
-        acc[2] += paged_exp2(v.z - ml.x) * ml.y; acc[3] += paged_exp2(v.w - ml.x) * ml.y;
-      }
+    #pragma unroll
+    for (int i = 0; i < QB; ++i) {
+      if (qa + i >= G) continue;
+      const float2 ml = sm_ml[i];
+      acc[0] += paged_exp2(v[i].x - ml.x) * ml.y; acc[1] += paged_exp2(v[i].y - ml.x) * ml.y;
+      acc[2] += paged_exp2(v[i].z - ml.x) * ml.y; acc[3] += paged_exp2(v[i].w - ml.x) * ml.y;
     }
   }
   const size_t at = (size_t)bh * a.c.table_pages * a.c.page_rows + row;

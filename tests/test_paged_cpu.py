@@ -19,22 +19,24 @@ HARNESS = r"""
 #include <vector>
 #include "paged_plan.h"
 using namespace amph;
-// The pieces of `wgs` workgroups over walks of the given steps (U a sequence): every step in one piece, every cut part in the place where
+// The pieces of the workgroups over walks of the given steps (U a sequence): every step in one piece, every cut part in the place where
 // the walk's list has it, no place used twice.  Returns 0, or the number of the rule that fails.
-extern "C" int deal(const int *steps, int n_seq, int U, int wgs) {
+extern "C" int deal(const int *steps, int n_seq, int U) {
+  const int wgs = PAGED_WGS;
   long long total = 0;
   std::vector<long long> first;
   for (int b = 0; b < n_seq; ++b) for (int u = 0; u < U; ++u) { first.push_back(total); total += steps[b]; }
-  const int chunk = paged_chunk(total, wgs);
-  if (chunk < 1 || chunk % PAGED_WAVES || (long long)chunk * wgs < total) return 1;
+  const PagedDeal d = paged_deal(total);
+  if (d.begin(0) != 0 || d.begin(wgs) < total) return 1;
   std::vector<int> seen(total, 0), place(2 * wgs, -1), at(2 * wgs, -1);
   for (int w = 0; w < wgs; ++w) {
-    long long pos = (long long)w * chunk;
+    const long long pos = d.begin(w), end = d.begin(w + 1) < total ? d.begin(w + 1) : total;
     if (pos >= total) continue;
+    if (end <= pos || d.piece(pos) != w || d.piece(end - 1) != w) return 7;
     int b = 0;
     long long before = 0;
     while (!(pos >= before * U && pos < (before + steps[b]) * (long long)U)) before += steps[b++];
-    int off = (int)(pos - before * U), u = off / steps[b], s = off % steps[b], left = (int)(chunk < total - pos ? chunk : total - pos);
+    int off = (int)(pos - before * U), u = off / steps[b], s = off % steps[b], left = (int)(end - pos);
     bool head = true;
     while (left > 0) {
       if (b >= n_seq || steps[b] <= 0) return 2;
@@ -53,11 +55,21 @@ extern "C" int deal(const int *steps, int n_seq, int U, int wgs) {
   int used = 0, listed = 0;
   for (int p : place) used += p >= 0;
   for (int b = 0; b < n_seq; ++b) for (int u = 0; u < U && steps[b] > 0; ++u) {
-    const PagedWalk wk = paged_walk(first[(long long)b * U + u], steps[b], chunk);
+    const PagedWalk wk = paged_walk(first[(long long)b * U + u], steps[b], d);
     if (wk.w0 == wk.w1) continue;
     for (int w = wk.w0; w <= wk.w1; ++w, ++listed) if (w >= wgs || place[wk.place(w)] != b * U + u) return 5;
   }
   return used == listed ? 0 : 6;
+}
+extern "C" int far() {
+  for (long long total : {(1ll << 32) - 1, (1ll << 32) + 77, (1ll << 36) - 3, (1ll << 36) - 511}) {
+    const PagedDeal d = paged_deal(total);
+    for (int w = 0; w < PAGED_WGS; ++w) {
+      const long long a = d.begin(w), b = d.begin(w + 1);
+      if (b <= a || d.piece(a) != w || d.piece(b - 1) != w || (w == PAGED_WGS - 1 && b != total)) return w + 1;
+    }
+  }
+  return 0;
 }
 extern "C" int rows(int len, int n_new, int valid, int cap) { return paged_rows(len, valid == -99 ? n_new : paged_new(n_new, valid), cap); }
 """
@@ -71,16 +83,21 @@ def plan(tmp_path_factory):
     return C.CDLL(str(d / "harness.so"))
 
 
-def deal(plan, steps, U, wgs):
-    return plan.deal((C.c_int * len(steps))(*steps), len(steps), U, wgs)
+def deal(plan, steps, U):
+    return plan.deal((C.c_int * len(steps))(*steps), len(steps), U)
 
 
-@pytest.mark.parametrize("steps,U,wgs", [
-    ([1], 1, 512), ([32], 32, 512), ([4096], 8, 512), ([0, 0, 5, 0], 4, 512), ([1] * 1024, 1, 512), ([0] * 1023 + [7], 3, 512),
-    ([100000], 1, 512), ([3, 0, 4096, 1, 0], 8, 512), ([129] * 64, 8, 512), ([5, 6], 2, 1),
+@pytest.mark.parametrize("steps,U", [
+    ([1], 1), ([32], 32), ([4096], 8), ([0, 0, 5, 0], 4), ([1] * 1024, 1), ([0] * 1023 + [7], 3), ([100000], 1), ([3, 0, 4096, 1, 0], 8),
+    ([129] * 64, 8), ([5, 6], 2), ([2047], 1), ([2048], 1), ([2049], 1), ([2559], 1), ([2560], 1), ([1] * 700, 40),
 ])
-def test_every_step_is_walked_once_and_found_again(plan, steps, U, wgs):
-    assert deal(plan, steps, U, wgs) == 0
+def test_every_step_is_walked_once_and_found_again(plan, steps, U):
+    assert deal(plan, steps, U) == 0
+
+
+def test_pieces_beyond_32_bits(plan):
+    """The most steps that a call can have, every piece's first and last step."""
+    assert plan.far() == 0
 
 
 def test_random_lengths_are_dealt_out(plan):
@@ -89,11 +106,11 @@ def test_random_lengths_are_dealt_out(plan):
         n = rng.choice([1, 2, 5, 33, 200])
         top = rng.choice([1, 9, 130, 2000 if n < 10 else 50])
         steps = [rng.choice([0, 1, top, rng.randint(0, top)]) for _ in range(n)]
-        assert deal(plan, steps, rng.choice([1, 2, 7, 40]), rng.choice([1, 3, 17, 256, 512])) == 0, steps
+        assert deal(plan, steps, rng.choice([1, 2, 7, 40])) == 0, steps
 
 
 def test_no_steps_at_all(plan):
-    assert deal(plan, [0, 0, 0], 4, 512) == 0
+    assert deal(plan, [0, 0, 0], 4) == 0
 
 
 @pytest.mark.parametrize("len_,n_new,valid,cap,expect", [
@@ -117,7 +134,7 @@ def fault(n_layers=1, cfg=None, null=False, **kw):
 
 def test_a_sound_cache_is_taken():
     assert fault() is None and fault(n_layers=0) is None and fault(max_pages=1, n_kv_heads=1, page_rows=32) is None
-    assert fault(n_seq=1024, table_pages=2 ** 18) is None and fault(layer_stride=0) is None
+    assert fault(n_seq=1024, table_pages=2 ** 18, max_pages=2 ** 18) is None and fault(layer_stride=0) is None
     assert fault(page_stride=2 ** 42, layer_stride=2 ** 45, n_layers=2) is None
     assert fault(cfg=base_cfg(dtype=B.AMPH_BF16)) is None
 
@@ -129,6 +146,7 @@ def test_a_sound_cache_is_taken():
     (dict(layer_stride=2), False), (dict(n_layers=-1), False),
     (dict(n_seq=1025), True), (dict(n_kv_heads=3), True), (dict(page_rows=48), True), (dict(page_rows=16), True), (dict(max_pages=5), True),
     (dict(table_pages=2 ** 18 + 1), True), (dict(page_stride=2 ** 43), True), (dict(head_stride=2 ** 46), True), (dict(layer_stride=2 ** 45, n_layers=3), True), (dict(n_layers=2 ** 30), True),
+    (dict(n_seq=1024, table_pages=2 ** 18, max_pages=2 ** 18, cfg=base_cfg(n_heads=128, d_model=8192)), True),
 ])
 def test_an_unsound_cache_is_refused(kw, shape):
     got = fault(**kw)

@@ -474,8 +474,12 @@ __global__ __launch_bounds__(256) void k_paged_fold(const PagedAttnArgs a, bool 
 
 int paged_query_blocks(int group) { return group > 16 ? 2 : 1; }
 
-// Up to this many key steps a wave walks by itself costs less than the launch of a fold.
-static bool paged_alone(const PagedAttnArgs &a, int kstep) { return a.seqs.cap <= 4 * PAGED_WAVES * kstep; }
+// A workgroup for every walk saves the launch of a fold, but a compute unit takes in some 60 GB/s, and unequal lengths are not evened out.  So:
+// while the longest walk that the bound allows has few steps, more of them where there are walks for half of the compute units.  Measured (us;
+// 32 query heads, bf16, 128 dims, alone / cut and joined): 32 walks of 512 rows 9.1 / 10.3, 768 10.9 / 10.4, 1024 13.3 / 11.2; 128 walks of 512
+// 10.4 / 14.4, 1024 16.0 / 18.6, 1536 22.1 / 23.7; 256 walks of 1024 23.3 / 28.5, 2048 43.3 / 48.2 (there the bound says too little about
+// lengths that differ).  Eight waves instead of four were no faster (32 walks of 1024 rows 13.8, 512 walks of 256 16.1 against 13.5).
+static bool paged_alone(const PagedAttnArgs &a, int walks, int kstep) { return a.seqs.cap <= (walks >= 128 ? 8 : 4) * PAGED_WAVES * kstep; }
 
 size_t paged_attn_ws_bytes(int n_seq, int n_heads, int n_kv, int d_h, int cap, bool weights, PagedAttnArgs *a, unsigned char *ws) {
   size_t at = 0;
@@ -495,7 +499,7 @@ static hipError_t paged_attn_shape(hipStream_t st, PagedAttnArgs a) {
   a.n_qg = (a.group + C::NQ - 1) / C::NQ;
   a.walks = a.c.n_kv * a.n_qg;
   const int walks = a.seqs.n_seq * a.walks;
-  const bool alone = paged_alone(a, C::KSTEP), weights = a.weights_out != nullptr;
+  const bool alone = paged_alone(a, walks, C::KSTEP), weights = a.weights_out != nullptr;
   if (alone)
     hipLaunchKernelGGL((k_paged_attn<T, DH, NQB, true>), dim3(walks), dim3(256), 0, st, a);
   else

@@ -715,7 +715,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   typedef int ij __attribute__((ext_vector_type(J), aligned(4)));
   extern __shared__ __align__(16) int sm_hole[];       // [most] places below the budget, ascending; [most] moves where they are made here (HELD)
   __shared__ int hist[BINS];
-  __shared__ __align__(16) int sm_new[NW], sm_a[NW], sm_b[NW], sm_c[NW], sm_d[NW], sm_e[NW];
+  __shared__ __align__(16) int sm_new[NW], sm_a[NW], sm_b[NW], sm_c[NW], sm_d[NW], sm_e[NW], sm_f[NW], sm_eq[NW];
   __shared__ int sm_pick[3], sm_few;
   __shared__ unsigned sm_key[FEW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, unit = blockIdx.x;
@@ -771,7 +771,16 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     if (bad) atomicOr(a.dev_status, (unsigned)(R < 0 ? AMPH_DEV_KV_OVERFLOW : AMPH_DEV_BAD_PAGE));
   }
   if (!bad && (a.weights_in != a.weights_out || a.pos_in != a.pos_out))               // elsewhere: all places first, then what moves
-    for (int i = tid; i < min(R, budget); i += NT) { w_out[i] = w[i]; pos_out[i] = pos[i]; }
+    lines([&](int, int row, const fj &x, const ij &p) {
+      const int end = min(R, budget);
+      if (row + J <= end) {
+        *reinterpret_cast<fj *>(w_out + row) = x;
+        *reinterpret_cast<ij *>(pos_out + row) = p;
+      } else {
+        #pragma unroll
+        for (int j = 0; j < J; ++j) if (row + j < end) { w_out[row + j] = x[j]; pos_out[row + j] = p[j]; }
+      }
+    });
   if (bad || R <= budget) {
     if (!a.fused && tid == 0) a.n_moves[unit] = 0;
     return;
@@ -837,33 +846,42 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     return;
   }
 
-  // ---- the smallest kept key: `want` of the keys in [lo, hi] are kept
-  unsigned lo = 0xffffffffu, hi = 0u;
-  int count = 0;                                       // of rows of any key but the lowest; of newest rows in the upper half
+  // ---- the smallest kept key: `want` of the keys in [lo, hi] are kept.  Weights are hardly ever negative, and often zero: the positive ones
+  // are a range of their own (many zeros would wait for one counter, and lie far from the smallest other weight)
+  constexpr unsigned ZERO = 0x80000000u;
+  unsigned lo = 0xffffffffu, lo_any = 0xffffffffu, hi = 0u;
+  int over_zero = 0, some_safe = 0;                    // rows above zero; of any key but the lowest, and of newest rows in the upper half
   keys([&](int, int, const uj &k) {
     #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const bool fixed = k[j] == 0xffffffffu;
-      count += (k[j] != 0u ? 1 : 0) + (fixed ? 0x10000 : 0);
-      lo = k[j] ? min(lo, k[j]) : lo;
+      const bool fixed = k[j] == 0xffffffffu, over = k[j] > ZERO;
+      over_zero += over ? 1 : 0;
+      some_safe += (k[j] != 0u ? 1 : 0) + (fixed ? 0x10000 : 0);
+      lo = over ? min(lo, k[j]) : lo;
+      lo_any = k[j] ? min(lo_any, k[j]) : lo_any;
       hi = fixed ? hi : max(hi, k[j]);
     }
   });
-  int some = count & 0xffff, safe = count >> 16;
-  some = wave_fold(some, AddI());
-  safe = wave_fold(safe, AddI());
+  const int over = wave_fold(over_zero, AddI());
+  int some = wave_fold(some_safe & 0xffff, AddI()), safe = wave_fold(some_safe >> 16, AddI());
   lo = wave_fold(lo, MinU());
+  lo_any = wave_fold(lo_any, MinU());
   hi = wave_fold(hi, MaxU());
-  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; sm_d[wave] = some; }
+  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; sm_d[wave] = some; sm_e[wave] = over; sm_f[wave] = (int)lo_any; }
   __syncthreads();
-  safe = some = 0;
+  safe = some = over_zero = 0;
   #pragma unroll
-  for (int i = 0; i < NW; ++i) { safe += sm_a[i]; some += sm_d[i]; lo = min(lo, (unsigned)sm_b[i]); hi = max(hi, (unsigned)sm_c[i]); }
+  for (int i = 0; i < NW; ++i) {
+    safe += sm_a[i]; some += sm_d[i]; over_zero += sm_e[i];
+    lo = min(lo, (unsigned)sm_b[i]); lo_any = min(lo_any, (unsigned)sm_f[i]); hi = max(hi, (unsigned)sm_c[i]);
+  }
   int want = budget - safe;
   bool all_equal = false;                              // all keys from lo on are kept
   if (want <= 0) { lo = 0xffffffffu; want = budget; }
   else if (some < budget) { lo = 0u; want = budget - some; }
+  else if (over_zero < budget && lo_any == ZERO) { lo = ZERO; want = budget - over_zero; }
   else {
+    if (over_zero < budget) { lo = lo_any; hi = ZERO; want = budget - over_zero; }
     for (;;) {
       const unsigned span = hi - lo;
       const int shift = span >> 11 ? 21 - __clz(span) : 0;             // (bins: span >> shift < 2048)
@@ -878,12 +896,12 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       #pragma unroll
       for (int i = 0; i < PB; ++i) { c[i] = hist[BINS - 1 - (tid * PB + i)]; mine += c[i]; }
       int upto = wave_scan(mine);
-      if (lane == WAVE - 1) sm_e[wave] = upto;
+      if (lane == WAVE - 1) sm_new[wave] = upto;
       __syncthreads();
       #pragma unroll
       for (int i = 0; i < PB; ++i) hist[BINS - 1 - (tid * PB + i)] = 0;
       int all;
-      upto += before(sm_e, all);
+      upto += before(sm_new, all);
       int above = upto - mine;
       if (upto >= want && above < want) {
         #pragma unroll
@@ -932,10 +950,10 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       for (int j = 0; j < J; ++j) eq += k[j] == from_key && row + j < R ? 1 : 0;
     });
     eq = wave_fold(eq, AddI());
-    if (lane == 0) sm_new[wave] = eq;                  // (what it held has been read by all since the barrier before)
+    if (lane == 0) sm_eq[wave] = eq;
     __syncthreads();
     int all;
-    eq = before(sm_new, all);
+    eq = before(sm_eq, all);
   }
   const int eq_before = eq;
   // the J rows that a lane keeps, as bits; all lanes, groups in order (eq: the equal keys before the group)

@@ -740,8 +740,6 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     #pragma unroll
     for (int g = 0; g < GROUPS; ++g) if (g < live_groups) load(g, wr[g], pr[g]);
   }
-  for (int i = tid; i < BINS; i += NT) hist[i] = 0;
-  if (tid == 0) sm_few = 0;
   bool bad = R < 0;
   for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += NT) bad |= (unsigned)row_table[i] >= (unsigned)a.c.n_pages;
   auto lines = [&](auto f) {                           // f(g, first row of the lane, J weights, J positions)
@@ -850,6 +848,8 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   // are a range of their own (many zeros would wait for one counter, and lie far from the smallest other weight)
   constexpr unsigned ZERO = 0x80000000u;
   unsigned lo = 0xffffffffu, lo_any = 0xffffffffu, hi = 0u;
+  for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+  if (tid == 0) sm_few = 0;
   int over_zero = 0, some_safe = 0;                    // rows above zero; of any key but the lowest, and of newest rows in the upper half
   keys([&](int, int, const uj &k) {
     #pragma unroll

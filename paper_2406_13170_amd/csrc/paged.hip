@@ -705,15 +705,15 @@ __device__ __forceinline__ void evict_move_rows(const PagedPages &c, const int32
 }
 
 // NT threads.  Rows are dealt in order to waves, groups, lanes, J to a lane; RPT > 0: a lane keeps the keys of its RPT rows in registers
-// (cap <= NT * RPT), 0: they are computed anew where they are needed.
+// (cap <= NT * RPT; up to 16 rows their weights and positions too), 0: they are computed anew where they are needed.
 template <typename T, int DH, int NT, int RPT>
 __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   constexpr int NW = NT / WAVE, BINS = 2048, FEW = 64;
-  constexpr bool HELD = RPT > 0;
+  constexpr bool HELD = RPT > 0, WHOLE = HELD && RPT <= 16;
   constexpr int J = HELD && RPT < 8 ? RPT : 8, GROUPS = HELD ? RPT / J : 1;
   typedef float fj __attribute__((ext_vector_type(J), aligned(4)));
   typedef int ij __attribute__((ext_vector_type(J), aligned(4)));
-  extern __shared__ __align__(16) int sm_hole[];       // [most] places below the budget, ascending; [most] moves where they are made here (HELD)
+  extern __shared__ __align__(16) int sm_hole[];       // [most] places below the budget, ascending; [most] moves where they are made here (WHOLE)
   __shared__ int hist[BINS];
   __shared__ __align__(16) int sm_new[NW], sm_a[NW], sm_b[NW], sm_c[NW], sm_d[NW], sm_e[NW], sm_f[NW], sm_eq[NW];
   __shared__ int sm_pick[3], sm_few;
@@ -733,26 +733,30 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     x = *reinterpret_cast<const fj *>(w + r);
     p = *reinterpret_cast<const ij *>(pos + r);
   };
-  fj wr[GROUPS];
-  ij pr[GROUPS];
+  fj wr[WHOLE ? GROUPS : 1];
+  ij pr[WHOLE ? GROUPS : 1];
   const int live_groups = R <= 0 ? 0 : min(groups, (R - 1 - wave * groups * WAVE * J + WAVE * J) / (WAVE * J));      // (may be negative)
-  if constexpr (HELD) {
+  if constexpr (WHOLE) {
     #pragma unroll
     for (int g = 0; g < GROUPS; ++g) if (g < live_groups) load(g, wr[g], pr[g]);
   }
   bool bad = R < 0;
   for (int i = tid; i < (max(R, 0) + a.c.page_rows - 1) / a.c.page_rows; i += NT) bad |= (unsigned)row_table[i] >= (unsigned)a.c.n_pages;
   auto lines = [&](auto f) {                           // f(g, first row of the lane, J weights, J positions)
-    if constexpr (HELD) {
+    auto one = [&](int g) {
+      fj x;
+      ij p;
+      load(g, x, p);
+      f(g, row_of(g), x, p);
+    };
+    if constexpr (WHOLE) {
       #pragma unroll
       for (int g = 0; g < GROUPS; ++g) if (g < live_groups) f(g, row_of(g), wr[g], pr[g]);
+    } else if constexpr (HELD) {
+      #pragma unroll
+      for (int g = 0; g < GROUPS; ++g) if (g < live_groups) one(g);
     } else {
-      for (int g = 0; g < live_groups; ++g) {
-        fj x;
-        ij p;
-        load(g, x, p);
-        f(g, row_of(g), x, p);
-      }
+      for (int g = 0; g < live_groups; ++g) one(g);
     }
   };
   int newest = INT32_MIN;
@@ -811,7 +815,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     return s;
   };
   int2 *moves = a.moves + (size_t)unit * a.most;
-  int2 *fused_moves = reinterpret_cast<int2 *>(sm_hole + (a.most + 1) / 2 * 2);      // (HELD)
+  int2 *fused_moves = reinterpret_cast<int2 *>(sm_hole + (a.most + 1) / 2 * 2);      // (WHOLE)
   const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
 
   if (R == budget + 1) {
@@ -1008,7 +1012,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     const int mine = __popc(m), upto = wave_scan(mine);
     for (int i = n_hole + upto - mine; m; m &= m - 1, ++i) {
       const int r = row + __builtin_ctz(m);
-      if constexpr (HELD) sm_hole[i] = r; else moves[i].x = r;
+      if constexpr (WHOLE) sm_hole[i] = r; else moves[i].x = r;
     }
     n_hole += __builtin_amdgcn_readlane(upto, WAVE - 1);
   });
@@ -1019,7 +1023,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     const int mine = __popc(m), upto = wave_scan(mine);
     for (int i = n_from + upto - mine; m; m &= m - 1, ++i) {
       const int r = row + __builtin_ctz(m);
-      if constexpr (HELD) {
+      if constexpr (WHOLE) {
         const int2 mv = make_int2(sm_hole[i], r);
         if (a.fused) fused_moves[i] = mv; else moves[i] = mv;
       } else {
@@ -1031,7 +1035,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   __syncthreads();
   for (int i = tid; i < total; i += NT) {              // (rows behind the budget, which nobody writes, to places below it)
     int2 mv;
-    if constexpr (HELD) { if (a.fused) mv = fused_moves[i]; else mv = moves[i]; } else mv = moves[i];
+    if constexpr (WHOLE) { if (a.fused) mv = fused_moves[i]; else mv = moves[i]; } else mv = moves[i];
     w_out[mv.x] = w[mv.y];
     pos_out[mv.x] = pos[mv.y];
   }
@@ -1040,7 +1044,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     return;
   }
   for (int i0 = wave * 16; i0 < total; i0 += NW * 16) {
-    if constexpr (HELD) evict_move_rows<T, DH>(a.c, row_table, base, fused_moves, i0, total);
+    if constexpr (WHOLE) evict_move_rows<T, DH>(a.c, row_table, base, fused_moves, i0, total);
     else evict_move_rows<T, DH>(a.c, row_table, base, moves, i0, total);
   }
 }
@@ -1084,11 +1088,13 @@ static hipError_t paged_evict_shape(hipStream_t st, PagedEvictArgs a, int n_laye
   a.fused = a.most <= EVICT_FUSED;
   const int cap = a.seqs.cap;
   const size_t lds = (size_t)a.most * (a.fused ? 12 : 4) + 8;
-  #define EVICT(NT, RPT) hipLaunchKernelGGL((k_evict<T, DH, NT, RPT>), dim3(units), dim3(NT), RPT ? lds : 0, st, a)
+  #define EVICT(NT, RPT) hipLaunchKernelGGL((k_evict<T, DH, NT, RPT>), dim3(units), dim3(NT), RPT && RPT <= 16 ? lds : 0, st, a)
   if (cap <= 512) EVICT(256, 2);
   else if (cap <= 2048) EVICT(256, 8);
   else if (cap <= 8192) EVICT(1024, 8);
   else if (cap <= 16384) EVICT(1024, 16);
+  else if (cap <= 32768) EVICT(1024, 32);
+  else if (cap <= 65536) EVICT(1024, 64);
   else EVICT(1024, 0);
   #undef EVICT
   if (!a.fused)

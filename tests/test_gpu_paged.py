@@ -449,6 +449,10 @@ def test_evict_long():
     evict_case("bf16", 1, 64, [9000, 40], 8999, 1, layers=1, page=128, weights="ties")
     evict_case("f32", 1, 64, [17000, 300], 400, 0, layers=1, page=256, in_place=True, weights="ties")
     evict_case("bf16", 1, 64, [16999], 16999, 3, layers=1, page=1024, in_place=True)
+    evict_case("bf16", 1, 64, [66000, 100], 20000, 500, layers=1, page=1024, in_place=True)
+    evict_case("bf16", 1, 64, [66000], 65990, 0, layers=1, page=1024, weights="ties")
+    evict_case("f32", 1, 64, [40000, 30000], 30000, 1, layers=1, page=1024, weights="wild", in_place=True)
+    evict_case("bf16", 1, 128, [32767, 9000], 16000, 7000, layers=1, page=1024, weights="ties", positions="mixed", in_place=True)
 
 
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])

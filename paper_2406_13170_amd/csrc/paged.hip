@@ -276,20 +276,38 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     return;
   }
 
-  // ---- the sequences' lengths and the steps before each, thread t for sequences PT t .. PT t + PT - 1
-  int all = 0;
-  long long first = 0, last = 0;
-  auto deal = [&](auto tag) {
-    constexpr int PT = decltype(tag)::value;
+  // ---- the sequences' lengths, the steps before each, and the sequence and walk that this piece begins in.  Up to 64 sequences every
+  // wave finds that by itself, a sequence a lane; beyond, thread t has sequences 4 t .. 4 t + 3.
+  const bool few = n_seq <= WAVE;
+  int all, L_lane = 0, b, at;
+  long long first, last;
+  if (few) {
+    if (lane < n_seq) L_lane = paged_len(a.seqs, lane);
+    const int st = L_lane > 0 ? (L_lane + KSTEP - 1) / KSTEP : 0, upto = wave_scan(st), before = upto - st;
+    all = __builtin_amdgcn_readlane(upto, WAVE - 1);
+    const PagedDeal pieces = paged_deal((long long)all * U);
+    first = pieces.begin(blockIdx.x);
+    last = pieces.begin(blockIdx.x + 1);
+    if (blockIdx.x == 0 && wave == 0 && lane < n_seq) {
+      a.plan[lane] = before;
+      a.plan[n_seq + 1 + lane] = L_lane;
+      if (L_lane < 0) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
+    }
+    const long long off = first - (long long)before * U;
+    const uint64_t here = __ballot(off >= 0 && off < (long long)st * U);
+    b = here ? __builtin_ctzll(here) : 0;
+    at = __builtin_amdgcn_readlane((int)off, b);
+  } else {
+    constexpr int PT = PAGED_MAX_SEQ / 256;
     int st[PT], sum = 0;
     bool over = false;
     #pragma unroll
     for (int i = 0; i < PT; ++i) {
-      const int b = tid * PT + i;
+      const int bi = tid * PT + i;
       int L = 0;
-      if (b < n_seq) {
-        L = paged_len(a.seqs, b);
-        sm_len[b] = L;
+      if (bi < n_seq) {
+        L = paged_len(a.seqs, bi);
+        sm_len[bi] = L;
         over |= L < 0;
       }
       st[i] = L > 0 ? (L + KSTEP - 1) / KSTEP : 0;
@@ -300,6 +318,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     if (blockIdx.x == 0 && over) atomicOr(a.dev_status, (unsigned)AMPH_DEV_KV_OVERFLOW);
     __syncthreads();
     int before = upto - sum;
+    all = 0;
     #pragma unroll
     for (int w = 0; w < PAGED_WAVES; ++w) { before += w < wave ? sm_sum[w] : 0; all += sm_sum[w]; }
     const PagedDeal pieces = paged_deal((long long)all * U);
@@ -307,36 +326,34 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     last = pieces.begin(blockIdx.x + 1);
     #pragma unroll
     for (int i = 0; i < PT; ++i) {
-      const int b = tid * PT + i;
-      if (b < n_seq) {
-        if (blockIdx.x == 0) { a.plan[b] = before; a.plan[n_seq + 1 + b] = sm_len[b]; }
+      const int bi = tid * PT + i;
+      if (bi < n_seq) {
+        if (blockIdx.x == 0) { a.plan[bi] = before; a.plan[n_seq + 1 + bi] = sm_len[bi]; }
         const long long off = first - (long long)before * U;
-        if (off >= 0 && off < (long long)st[i] * U) { sm_at[0] = b; sm_at[1] = (int)off; }
+        if (off >= 0 && off < (long long)st[i] * U) { sm_at[0] = bi; sm_at[1] = (int)off; }
       }
       before += st[i];
     }
-  };
-  if (n_seq <= 256) deal(Rows<1>{}); else deal(Rows<PAGED_MAX_SEQ / 256>{});
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(sm_at[0]);
+    at = __builtin_amdgcn_readfirstlane(sm_at[1]);
+  }
   const long long total = (long long)all * U;
   if (blockIdx.x == 0 && tid == 0) a.plan[n_seq] = all;
-  if (first >= total) return;                          // (whole workgroup)
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(sm_at[0]), u, s, left = __builtin_amdgcn_readfirstlane((int)(min(last, total) - first));
+  if (first >= total) return;                          // (whole workgroup; what b and at are then is not looked at)
+  auto len_of = [&](int i) { return few ? __builtin_amdgcn_readlane(L_lane, i) : __builtin_amdgcn_readfirstlane(sm_len[i]); };
+  int L = len_of(b), left = __builtin_amdgcn_readfirstlane((int)(min(last, total) - first));
+  int u = at / ((L + KSTEP - 1) / KSTEP), s = at - u * ((L + KSTEP - 1) / KSTEP);
   bool head_of_piece = true;
-  {
-    const int steps = (__builtin_amdgcn_readfirstlane(sm_len[b]) + KSTEP - 1) / KSTEP, at = __builtin_amdgcn_readfirstlane(sm_at[1]);
-    u = at / steps;
-    s = at - u * steps;
-  }
   while (left > 0) {
-    const int L = __builtin_amdgcn_readfirstlane(sm_len[b]), steps = (L + KSTEP - 1) / KSTEP, n = min(steps - s, left);
+    const int steps = (L + KSTEP - 1) / KSTEP, n = min(steps - s, left);
     walk(b, u, L, s, n, n == steps, 2 * blockIdx.x + (head_of_piece ? 0 : 1));
     head_of_piece = false;
     left -= n;
     s = 0;
     if (++u == U) {
       u = 0;
-      do ++b; while (left > 0 && sm_len[b] <= 0);      // (steps are left: so is a sequence that has them)
+      while (left > 0 && (L = len_of(++b)) <= 0) {}    // (steps are left: so is a sequence that has them)
     }
   }
 }

@@ -70,7 +70,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
 
   // ---- the key steps [s, s + n) of one walk
   auto walk = [&](int b, int u, int L, int s, int n, bool whole, int place) {
-    const int h = u / n_qg, q_base = (u % n_qg) * NQ, live_q = min(G - q_base, NQ);
+    // this wave's steps are s + wave + 4 i, i < n_w; lane l finds where step 64 * block + l begins (bytes into the pages)
+    const int32_t *row_table = a.c.table + (size_t)b * a.c.table_pages;
+    const int n_w = (n - wave + PAGED_WAVES - 1) / PAGED_WAVES;
+    auto step_of = [&](int i0) { return max(min(s + wave + PAGED_WAVES * min(i0 + lane, n_w - 1), s + n - 1), 0); };   // (idle waves: any of the walk's)
+    int id = row_table[step_of(0) / psteps];           // asked for ahead of all else
+    const int h = u / n_qg, q_base = (u - h * n_qg) * NQ, live_q = min(G - q_base, NQ);
     const T *qb0 = (const T *)a.q + (size_t)b * a.ld_q + ((size_t)h * G + q_base) * DH;
     uint4 Qf[NQB][DSTEPS];                             // queries as B fragments: lane = query r16 of block qb
     #pragma unroll
@@ -83,7 +88,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     unsigned char *Kh = (unsigned char *)a.c.k + (size_t)h * a.c.head_stride * sizeof(T);
     unsigned char *Vh = (unsigned char *)a.c.v + (size_t)h * a.c.head_stride * sizeof(T);
     const int lane_at = r16 * 64 + g * 16;
-    const int32_t *row_table = a.c.table + (size_t)b * a.c.table_pages;
     float *score = a.scores ? a.scores + ((size_t)b * a.n_heads + (size_t)h * G + q_base) * a.seqs.cap : nullptr;
 
     f32x4 O[NQB][DB];
@@ -96,13 +100,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
     }
     bool bad = false;
 
-    // this wave's steps are s + wave + 4 i, i < n_w; lane l keeps where step 64 * block + l begins (bytes into the pages)
-    const int n_w = (n - wave + PAGED_WAVES - 1) / PAGED_WAVES;
     unsigned long long where = 0;
     auto look_up = [&](int i0) {
-      const int st = s + wave + PAGED_WAVES * min(i0 + lane, n_w - 1), pg = st / psteps;
-      int id = row_table[pg];
-      if ((unsigned)id >= (unsigned)a.c.n_pages) { bad = true; id = 0; }
+      const int st = step_of(i0), pg = st / psteps;
+      if ((unsigned)id >= (unsigned)a.c.n_pages) { bad = n_w > 0; id = 0; }
       where = ((unsigned long long)id * a.c.page_stride + (unsigned long long)(st - pg * psteps) * (KSTEP * DH)) * sizeof(T);
     };
     auto step_base = [&](int i) -> size_t {            // (uniform)
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
       #pragma unroll 1
       for (int i = 0; i < n_w; ++i) {
         const bool more = i + 1 < n_w;
-        if (more && ((i + 1) & 63) == 0) look_up(i + 1);
+        if (more && ((i + 1) & 63) == 0) { id = row_table[step_of(i + 1) / psteps]; look_up(i + 1); }
         at = step_base(i + 1);
         float sv[NQB][PER], pv[NQB][PER];
         scores(i, sv);

@@ -45,18 +45,21 @@ def attn_case(dtype, heads, n_kv, dim, lens, page=32, per=None, weights=None, la
                         workspace(ctx, pool.kv, 1 if weights else 0))
     torch.cuda.synchronize()
     assert ctx.device_status() == 0
-    worst = 0.0
+    worst, off, rounding, norm = 0.0, 0.0, 0.0, 0.0
     for b, L in enumerate(lens):
         ref, w, mag, reach = pr.attn(q[b, :heads * dim].view(heads, dim), pool.rows_k[layer][b], pool.rows_v[layer][b])
         err, most = (out[b].cpu().to(F64) - ref).abs(), pr.attn_bounds(dtype, ref, mag, reach, L, dim)
         assert bool((err <= most).all()), (b, L, float((err / most).max()))
         worst = max(worst, float((err / most).max()))
+        off, rounding, norm = (x + float(y.square().sum()) for x, y in ((off, err), (rounding, ref.to(tdt).to(F64) - ref), (norm, ref)))
         if weights:
             want = w + (w_in[b, :, :L].to(F64) if w_in is not None else 0.0)
             err, most = (w_out[b, :, :L].cpu().to(F64) - want).abs(), pr.weight_bounds(w, reach, n_kv, L, dim) + 2.0 ** -23 * want.abs()
             assert bool((err <= most).all()), (b, L)
             assert bool((w_out[b, :, L:] == -3.0).all())
-    say(f"  {dtype} {heads}/{n_kv} x {dim}, rows {lens[:6]}: {worst:.2f} of the bound")
+    # As a whole it is the output's rounding that counts: P has 16 bits and the sums 24, and their errors have either sign.
+    assert math.sqrt(off) <= 1.05 * math.sqrt(rounding) + (2.0 ** -15 if dtype == "bf16" else 2.0 ** -17) * math.sqrt(norm)
+    say(f"  {dtype} {heads}/{n_kv} x {dim}, rows {lens[:6]}: {worst:.2f} of the bound, error {math.sqrt(off / max(norm, 1e-300)):.1e}")
     return out
 
 
@@ -90,6 +93,8 @@ def test_attention_of_many_sequences():
     lens[0], lens[500], lens[1023] = 0, 900, 33
     attn_case("bf16", 2, 1, 64, lens, per=29)
     attn_case("f32", 4, 4, 64, [(b * b) % 90 for b in range(300)], weights="add")
+    for n in (63, 64, 65, 256, 257):
+        attn_case("bf16", 2, 1, 64, [(13 * b) % 40 for b in range(n - 1)] + [700], weights="new", per=22)
 
 
 def test_attention_of_every_sequence_empty():
@@ -245,6 +250,26 @@ def test_attention_beyond_32_bits():
     ctx.amph_paged_evict(kv, 1, 250, 1, 1, None, i32([250]), n, w, w, pos, pos, workspace(ctx, kv, 1))
     assert int(n) == 250 and ctx.device_status() == 0
     assert torch.equal(lr.tiled_to_keys(k[0, ids[0], 0].cpu())[3], new[0, 0]) and torch.equal(lr.tiled_to_values(v[0, ids[0], 0].cpu())[3], new[0, 0])
+
+
+def test_attention_over_the_most_rows():
+    """2^24 rows: keys that are all the same, so that the output is the values' mean and every row has the same weight."""
+    L, page, dim = 1 << 24, 1 << 14, 64
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k = torch.zeros(1, L // page, 1, page, dim, dtype=torch.bfloat16, device=DEV)
+    v = torch.randn(k.shape, dtype=torch.bfloat16, device=DEV, generator=g) + 1.0
+    table = torch.randperm(L // page, device=DEV, generator=g).to(torch.int32).view(1, -1).contiguous()
+    kv, ctx = D.paged_pool(k, v, table), pr.make_ctx("bf16", 2, dim)
+    out, w = torch.zeros(1, 2, dim, device=DEV, dtype=torch.bfloat16), torch.zeros(1, 1, L, device=DEV)
+    q = torch.randn(1, 2, dim, device=DEV, dtype=torch.bfloat16)
+    ctx.amph_paged_attn(kv, 0, q, 2 * dim, 1, None, i32([L - 1]), out, None, w, workspace(ctx, kv, 1))
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    mean = v.view(-1, dim // 16, 16, 32).double().mean((0, 3)).view(dim).cpu()          # [step, block of dims, dim, row of the step]
+    mag = v.view(-1, dim // 16, 16, 32).float().abs().mean((0, 3)).view(dim).double().cpu()
+    # 512 pieces of four waves, 256 key steps each, one sum after the other: (256 + 4 + 512) sums with a step of 2^-23 each
+    assert bool(((out[0].cpu().double() - mean).abs() <= 2.0 ** -8 * mean.abs() + mag * (2.0 ** -16 + 800 * 2.0 ** -22)).all())
+    assert bool(((w * (L / 2) - 1).abs() <= 800 * 2.0 ** -22).all())
 
 
 @pytest.mark.parametrize("cfg,L", [(si.MINI, 77), (si.MINI, 700), (si.TINY, 130)])
@@ -632,6 +657,49 @@ def test_two_streams_with_workspaces_of_their_own():
         torch.cuda.synchronize()
         for graph, stream, out, w, want, _ in sides:
             assert torch.equal(out, want[0]) and torch.equal(w, want[1])
+
+
+def test_graphs_that_share_a_workspace():
+    """An attention with weights and an eviction, captured apart over one workspace, replayed in turn on one stream with eager calls in between:
+    nothing of a call is left there for the next."""
+    pools = [Pool("bf16", 2, 128, 64, lens, 20, seed=i) for i, lens in enumerate(([1200, 60], [300, 1100]))]
+    ctx, n = pr.make_ctx("bf16", 8, 128), [i32([1200, 60]), i32([300, 1100])]
+    ws, q = workspace(ctx, pools[0].kv, 1), torch.randn(2, 8, 128, device=DEV).to(torch.bfloat16)
+    outs, ws_w = [torch.zeros_like(q) for _ in range(2)], [torch.zeros(1, 2, 2, 1280, device=DEV) for _ in range(2)]
+    pos, kept = torch.arange(1280, device=DEV, dtype=torch.int32).expand(1, 2, 2, 1280).contiguous(), [torch.zeros(1, 2, 2, 1280, device=DEV) for _ in range(2)]
+    places, left = [torch.zeros_like(pos) for _ in range(2)], [i32([0, 0]) for _ in range(2)]
+    mass = torch.rand(1, 2, 2, 1280, device=DEV)                      # what the evictions go by: the same in every pass
+
+    def attend(i):
+        ctx.amph_paged_attn(pools[i].kv, 0, q, 1024, 0, None, n[i], outs[i], None, ws_w[i], ws)
+
+    def drop(i):
+        ctx.amph_paged_evict(pools[i].kv, 1, 256, 10, 0, None, n[i], left[i], mass, kept[i], pos, places[i], ws)
+    attend(0), attend(1), drop(0), drop(1)
+    torch.cuda.synchronize()
+    # (rows moved below the budget: from here on every pass sees the same caches, as the same rows move to the same places again)
+    attend(0), attend(1), drop(0), drop(1)
+    torch.cuda.synchronize()
+    want = [x.clone() for x in outs + ws_w + kept + places + left]
+    stream, graphs = torch.cuda.Stream(), []
+    ctx.set_stream(stream.cuda_stream)
+    for call, i in ((attend, 0), (attend, 1), (drop, 0), (drop, 1)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call(i)
+        graphs.append(graph)
+    for turn in range(4):
+        with torch.cuda.stream(stream):
+            for x in outs + kept + places:
+                x.zero_()
+            for graph in graphs:
+                graph.replay()
+            if turn % 2:
+                attend(1)
+        torch.cuda.synchronize()
+        for x, y in zip(outs + ws_w + kept + places + left, want):
+            assert torch.equal(x, y), turn
+    assert ctx.device_status() == 0
 
 
 def test_refusals():

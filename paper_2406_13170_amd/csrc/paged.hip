@@ -188,17 +188,24 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a) {
       }
       #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
-        const uint4 Pf = pack16<T>(pv[qb]);
-        #pragma unroll
-        for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Pf, O[qb][db]);
-        if constexpr (sizeof(T) == 2) {                // what the rounding to bf16 took away, as a second operand: P has 16 bits
-          float hi[PER], rest[PER];
-          Elem<T>::unpack(Pf, hi);
+        if constexpr (sizeof(T) == 2) {
+          // P in two operands, 16 bits: its upper half as it is, and what that leaves out, which is not negative, nor zero (an infinite value
+          // times zero would be NaN; 2^-100 of a finite one is nothing)
+          float rest[PER];
+          unsigned hi[PER / 2];
           #pragma unroll
-          for (int j = 0; j < PER; ++j) rest[j] = pv[qb][j] - hi[j];
-          const uint4 Rf = pack16<T>(rest);
+          for (int j = 0; j < PER; ++j) rest[j] = fmaxf(pv[qb][j] - __uint_as_float(__float_as_uint(pv[qb][j]) & 0xffff0000u), 7.8886091e-31f);
+          #pragma unroll
+          for (int j = 0; j < PER / 2; ++j) hi[j] = __builtin_amdgcn_perm(__float_as_uint(pv[qb][2 * j + 1]), __float_as_uint(pv[qb][2 * j]), 0x07060302u);
+          const uint4 Pf = make_uint4(hi[0], hi[1], hi[PER / 2 - 2], hi[PER / 2 - 1]), Rf = pack16<T>(rest);
+          #pragma unroll
+          for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Pf, O[qb][db]);
           #pragma unroll
           for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Rf, O[qb][db]);
+        } else {
+          const uint4 Pf = pack16<T>(pv[qb]);
+          #pragma unroll
+          for (int db = 0; db < DB; ++db) O[qb][db] = mma16<T>(Vf[db], Pf, O[qb][db]);
         }
       }
     };

@@ -139,35 +139,38 @@ def test_attention_new_rows_count():
     assert ctx.device_status() == 0                       # (the third sequence then has rows of NaN, which are rows)
 
 
-def test_attention_special_values():
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_special_values(dtype):
     """NaN and infinities in a row's key or value reach that sequence's head alone; a score of -inf has no weight; rows all of -inf give
     zeros."""
     lens = [100, 100, 100, 100, 90]
-    pool, ctx = Pool("f32", 2, 64, 32, lens, 40), pr.make_ctx("f32", 2, 64)
+    pool, ctx, tdt = Pool(dtype, 2, 64, 32, lens, 40), pr.make_ctx(dtype, 2, 64), D.torch_dtype(dtype)
 
     def put(x, back, to, b, h, row, value):
         rows = back(x[0, pool.table[b].long().to(DEV)].cpu())           # [per, n_kv, page, dim]
         rows[row // 32, h, row % 32] = value
         x[0, pool.table[b].long().to(DEV)] = to(rows).to(DEV)
-    q = torch.ones(5, 2, 64, device=DEV)
+    q = torch.ones(5, 2, 64, device=DEV, dtype=tdt)
     put(pool.k, lr.tiled_to_keys, lr.keys_to_tiled, 0, 0, 7, math.nan)
     put(pool.v, lr.tiled_to_values, lr.values_to_tiled, 1, 1, 99, math.inf)
+    put(pool.v, lr.tiled_to_values, lr.values_to_tiled, 4, 0, 0, -math.inf)
     put(pool.k, lr.tiled_to_keys, lr.keys_to_tiled, 2, 0, 50, -math.inf)
     for r in range(100):
         put(pool.k, lr.tiled_to_keys, lr.keys_to_tiled, 3, 1, r, -math.inf)
-    out, w = torch.zeros(5, 2, 64, device=DEV), torch.zeros(5, 2, pool.cap, device=DEV)
+    out, w = torch.zeros(5, 2, 64, device=DEV, dtype=tdt), torch.zeros(5, 2, pool.cap, device=DEV)
     for most in (pool.per, 4):                             # the keys dealt out, and one workgroup a head
         pool.kv.max_pages = most
         ctx.amph_paged_attn(pool.kv, 0, q, 128, 0, None, i32(lens), out, None, w, workspace(ctx, pool.kv, 1))
         torch.cuda.synchronize()
         assert ctx.device_status() == 0
         assert out[0, 0].isnan().all() and out[0, 1].isfinite().all() and w[0, 0, :100].isnan().all()
-        assert out[1, 1].isinf().all() and out[1, 0].isfinite().all()
+        assert bool((out[1, 1] == math.inf).all()) and out[1, 0].isfinite().all()
+        assert bool((out[4, 0] == -math.inf).all()) and out[4, 1].isfinite().all()
         keep = [r for r in range(100) if r != 50]
         ref = pr.attn(q[2, :1].cpu(), pool.rows_k[0][2][:1, keep], pool.rows_v[0][2][:1, keep])
-        assert bool(((out[2, :1].cpu().to(F64) - ref[0]).abs() <= pr.attn_bounds("f32", ref[0], ref[2], ref[3], 100, 64)).all())
+        assert bool(((out[2, :1].cpu().to(F64) - ref[0]).abs() <= pr.attn_bounds(dtype, ref[0], ref[2], ref[3], 100, 64)).all())
         assert float(w[2, 0, 50]) == 0.0 and out[2].isfinite().all()
-        assert bool((out[3, 1] == 0).all()) and bool((w[3, 1, :100] == 0).all()) and out[4].isfinite().all()
+        assert bool((out[3, 1] == 0).all()) and bool((w[3, 1, :100] == 0).all())
 
 
 def test_attention_bad_lengths_and_pages():
@@ -467,6 +470,8 @@ def test_evict(dtype, dim, lens, budget, recent):
 def test_evict_equal_and_special_weights(weights, positions):
     evict_case("bf16", 2, 64, [700, 260], 257, 40, weights=weights, positions=positions, seed=3)
     evict_case("f32", 2, 64, [130, 64], 100, 100, weights=weights, positions=positions, in_place=True)
+    evict_case("bf16", 2, 64, [256, 255], 256, 9, weights=weights, positions=positions, in_place=True)
+    evict_case("bf16", 2, 128, [700], 700, 0, weights=weights, positions=positions, seed=5)
 
 
 def test_evict_long():

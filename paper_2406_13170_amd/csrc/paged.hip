@@ -741,6 +741,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   extern __shared__ __align__(16) int sm_hole[];       // [most] places below the budget, ascending; [most] moves where they are made here (WHOLE)
   __shared__ int hist[BINS];
   __shared__ __align__(16) int sm_new[NW], sm_a[NW], sm_b[NW], sm_c[NW], sm_d[NW], sm_e[NW], sm_f[NW], sm_eq[NW];
+  static_assert(NW <= 16, "a row of lanes has a value of every wave");
   __shared__ int sm_pick[3], sm_few;
   __shared__ unsigned sm_key[FEW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, unit = blockIdx.x;
@@ -784,6 +785,14 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       for (int g = 0; g < live_groups; ++g) one(g);
     }
   };
+  // op over the waves' values, in every lane
+  auto across = [&](const int *sm, auto op, auto none) {
+    auto v = (lane & 15) < NW ? (decltype(none))sm[lane & 15] : none;
+    v = op(v, lanes_ror<8>(v));
+    v = op(v, lanes_ror<4>(v));
+    v = op(v, lanes_ror<2>(v));
+    return op(v, lanes_ror<1>(v));
+  };
   int newest = INT32_MIN;
   lines([&](int, int row, const fj &, const ij &p) {
     #pragma unroll
@@ -812,8 +821,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     if (!a.fused && tid == 0) a.n_moves[unit] = 0;
     return;
   }
-  #pragma unroll
-  for (int i = 0; i < NW; ++i) newest = max(newest, sm_new[i]);
+  newest = across(sm_new, MaxI(), (int)INT32_MIN);
   const long long safe_from = (long long)newest - a.recent;           // positions above it are kept first
   auto key_of = [&](float x, int p) -> unsigned { return (long long)p > safe_from ? 0xffffffffu : rank_key(x); };
   typedef unsigned uj __attribute__((ext_vector_type(J)));
@@ -831,13 +839,11 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       lines([&](int g, int row, const fj &x, const ij &p) { uj k; line_keys(row, x, p, k); f(g, row, k); });
     }
   };
-  // sums over the waves before this one, and over all
+  // a sum over the waves before this one, and over all
   auto before = [&](const int *sm, int &all) {
-    int s = 0;
-    all = 0;
-    #pragma unroll
-    for (int i = 0; i < NW; ++i) { const int v = sm[i]; s += i < wave ? v : 0; all += v; }
-    return s;
+    const int v = lane < NW ? sm[lane] : 0, s = wave_scan(v);
+    all = __builtin_amdgcn_readlane(s, WAVE - 1);
+    return __builtin_amdgcn_readlane(s, wave) - __builtin_amdgcn_readlane(v, wave);
   };
   int2 *moves = a.moves + (size_t)unit * a.most;
   int2 *fused_moves = reinterpret_cast<int2 *>(sm_hole + (a.most + 1) / 2 * 2);      // (WHOLE)
@@ -864,7 +870,7 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     for (int i = 0; i < NW; ++i)
       if (sm_c[i] >= 0 && (unsigned)sm_b[i] <= least) { least = (unsigned)sm_b[i]; gone = sm_c[i]; }
     const int2 one = make_int2(gone, budget);
-    if (tid == 0 && gone < budget) { w_out[gone] = w[budget]; pos_out[gone] = pos[budget]; }
+    if (tid == 0 && a.fused && gone < budget) { w_out[gone] = w[budget]; pos_out[gone] = pos[budget]; }
     if (!a.fused) {
       if (tid == 0) { moves[0] = one; a.n_moves[unit] = gone < budget; }
     } else if (wave == 0 && gone < budget) {
@@ -876,41 +882,52 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   // ---- the smallest kept key: `want` of the keys in [lo, hi] are kept.  Weights are hardly ever negative, and often zero: the positive ones
   // are a range of their own (many zeros would wait for one counter, and lie far from the smallest other weight)
   constexpr unsigned ZERO = 0x80000000u;
-  unsigned lo = 0xffffffffu, lo_any = 0xffffffffu, hi = 0u;
+  unsigned lo = 0xffffffffu, hi = 0u;
   for (int i = tid; i < BINS; i += NT) hist[i] = 0;
   if (tid == 0) sm_few = 0;
-  int over_zero = 0, some_safe = 0;                    // rows above zero; of any key but the lowest, and of newest rows in the upper half
+  int over_zero = 0, safe = 0;                         // rows above zero, and newest ones
   keys([&](int, int, const uj &k) {
     #pragma unroll
     for (int j = 0; j < J; ++j) {
       const bool fixed = k[j] == 0xffffffffu, over = k[j] > ZERO;
       over_zero += over ? 1 : 0;
-      some_safe += (k[j] != 0u ? 1 : 0) + (fixed ? 0x10000 : 0);
+      safe += fixed ? 1 : 0;
       lo = over ? min(lo, k[j]) : lo;
-      lo_any = k[j] ? min(lo_any, k[j]) : lo_any;
       hi = fixed ? hi : max(hi, k[j]);
     }
   });
-  const int over = wave_fold(over_zero, AddI());
-  int some = wave_fold(some_safe & 0xffff, AddI()), safe = wave_fold(some_safe >> 16, AddI());
+  over_zero = wave_fold(over_zero, AddI());
+  safe = wave_fold(safe, AddI());
   lo = wave_fold(lo, MinU());
-  lo_any = wave_fold(lo_any, MinU());
   hi = wave_fold(hi, MaxU());
-  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; sm_d[wave] = some; sm_e[wave] = over; sm_f[wave] = (int)lo_any; }
+  if (lane == 0) { sm_a[wave] = safe; sm_b[wave] = (int)lo; sm_c[wave] = (int)hi; sm_e[wave] = over_zero; }
   __syncthreads();
-  safe = some = over_zero = 0;
-  #pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    safe += sm_a[i]; some += sm_d[i]; over_zero += sm_e[i];
-    lo = min(lo, (unsigned)sm_b[i]); lo_any = min(lo_any, (unsigned)sm_f[i]); hi = max(hi, (unsigned)sm_c[i]);
-  }
+  safe = across(sm_a, AddI(), 0);
+  over_zero = across(sm_e, AddI(), 0);
+  lo = across(sm_b, MinU(), 0xffffffffu);
+  hi = across(sm_c, MaxU(), 0u);
   int want = budget - safe;
   bool all_equal = false;                              // all keys from lo on are kept
-  if (want <= 0) { lo = 0xffffffffu; want = budget; }
-  else if (some < budget) { lo = 0u; want = budget - some; }
-  else if (over_zero < budget && lo_any == ZERO) { lo = ZERO; want = budget - over_zero; }
-  else {
-    if (over_zero < budget) { lo = lo_any; hi = ZERO; want = budget - over_zero; }
+  bool search = true;
+  if (want <= 0) { lo = 0xffffffffu; want = budget; search = false; }
+  else if (over_zero < budget) {                       // zero weights, negative ones or NaN are kept too
+    int some = 0;                                      // rows of any key but the lowest
+    lo = 0xffffffffu;
+    hi = ZERO;
+    keys([&](int, int, const uj &k) {
+      #pragma unroll
+      for (int j = 0; j < J; ++j) { some += k[j] != 0u ? 1 : 0; lo = k[j] ? min(lo, k[j]) : lo; }
+    });
+    some = wave_fold(some, AddI());
+    lo = wave_fold(lo, MinU());
+    if (lane == 0) { sm_d[wave] = some; sm_f[wave] = (int)lo; }
+    __syncthreads();
+    some = across(sm_d, AddI(), 0);
+    lo = across(sm_f, MinU(), 0xffffffffu);
+    if (some < budget) { lo = 0u; want = budget - some; search = false; }
+    else { want = budget - over_zero; search = lo != ZERO; }
+  }
+  if (search) {
     for (;;) {
       const unsigned span = hi - lo;
       const int shift = span >> 11 ? 21 - __clz(span) : 0;             // (bins: span >> shift < 2048)
@@ -947,25 +964,31 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
       all_equal = in_bin == want;
       if (shift == 0 || all_equal) break;
       if (in_bin <= FEW) {
-        // ---- few keys left: every wave ranks them all; the want-th largest, and how many are larger
+        // ---- few keys left: one wave ranks them; the want-th largest, and how many are larger
         const unsigned few_span = hi - lo;
         keys([&](int, int, const uj &k) {
           #pragma unroll
           for (int j = 0; j < J; ++j) if (k[j] - lo <= few_span) sm_key[atomicAdd(&sm_few, 1)] = k[j];
         });
         __syncthreads();
-        const unsigned own = lane < in_bin ? sm_key[lane] : 0u;        // (in the order they came: only their values count)
-        int larger = 0, same = 0;
-        for (int s = 0; s < in_bin; ++s) {
-          const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)own, s);
-          larger += o > own ? 1 : 0;
-          same += o == own ? 1 : 0;
+        if (wave == 0) {
+          const unsigned own = lane < in_bin ? sm_key[lane] : 0u;      // (in the order they came: only their values count)
+          int larger = 0, same = 0;
+          for (int s = 0; s < in_bin; ++s) {
+            const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)own, s);
+            larger += o > own ? 1 : 0;
+            same += o == own ? 1 : 0;
+          }
+          if (lane < in_bin && larger < want && larger + same >= want) {       // (lanes of the same key write the same)
+            sm_pick[0] = (int)own;
+            sm_pick[1] = want - larger;
+            sm_pick[2] = same;
+          }
         }
-        const uint64_t at_want = __ballot(lane < in_bin && larger < want && larger + same >= want);
-        const int l = __builtin_ctzll(at_want);
-        lo = (unsigned)__builtin_amdgcn_readlane((int)own, l);
-        want -= __builtin_amdgcn_readlane(larger, l);
-        all_equal = want == __builtin_amdgcn_readlane(same, l);
+        __syncthreads();
+        lo = (unsigned)sm_pick[0];
+        want = sm_pick[1];
+        all_equal = sm_pick[2] == want;
         break;
       }
     }
@@ -1057,16 +1080,16 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
     }
     n_from += __builtin_amdgcn_readlane(upto, WAVE - 1);
   });
+  if (!a.fused) {                                      // k_evict_move makes them
+    if (tid == 0) a.n_moves[unit] = total;
+    return;
+  }
   __syncthreads();
   for (int i = tid; i < total; i += NT) {              // (rows behind the budget, which nobody writes, to places below it)
     int2 mv;
-    if constexpr (WHOLE) { if (a.fused) mv = fused_moves[i]; else mv = moves[i]; } else mv = moves[i];
+    if constexpr (WHOLE) mv = fused_moves[i]; else mv = moves[i];
     w_out[mv.x] = w[mv.y];
     pos_out[mv.x] = pos[mv.y];
-  }
-  if (!a.fused) {
-    if (tid == 0) a.n_moves[unit] = total;
-    return;
   }
   for (int i0 = wave * 16; i0 < total; i0 += NW * 16) {
     if constexpr (WHOLE) evict_move_rows<T, DH>(a.c, row_table, base, fused_moves, i0, total);
@@ -1081,14 +1104,22 @@ constexpr int EVICT_MOVES = 64;                        // moves of a workgroup: 
 // 60 MB of lines): 16.3 us.  (Whole steps through LDS, where the rows change places: 16.8 and 18.0 us, a wave for all dims and for a quarter.)
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a, int32_t *kv_len_out) {
-  const int tid = threadIdx.x, wave = tid >> 6, unit = blockIdx.x;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;
   const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
   if (!a.kv_len_out && h == 0 && layer == 0 && blockIdx.y == 0 && tid == 0) kv_len_out[b] = a.new_len[b];
   if (a.fused) return;
   const int n = a.n_moves[unit];
   const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
-  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES)
-    evict_move_rows<T, DH>(a.c, a.c.table + (size_t)b * a.c.table_pages, base, a.moves + (size_t)unit * a.most, i0, n);
+  const int2 *moves = a.moves + (size_t)unit * a.most;
+  const size_t at = (size_t)unit * a.c.table_pages * a.c.page_rows;
+  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES) {
+    if (lane < 16 && i0 + lane < n) {
+      const int2 mv = moves[i0 + lane];
+      a.weights_out[at + mv.x] = a.weights_in[at + mv.y];
+      a.pos_out[at + mv.x] = a.pos_in[at + mv.y];
+    }
+    evict_move_rows<T, DH>(a.c, a.c.table + (size_t)b * a.c.table_pages, base, moves, i0, n);
+  }
 }
 
 // Up to so many moves a head the workgroup that chose them makes them itself.

@@ -688,8 +688,7 @@ template hipError_t launch_paged_append<bf16_t>(hipStream_t, const PagedAppendAr
 //   the bin that holds it the same way (spread over the range, the counters are hit by few lanes at once, however close the
 //   exponents are).  Then the rows in their order: of equal keys the lowest are kept, the i-th kept row behind the budget gets the
 //   i-th dropped place below it.  A step that drops one row (a cache at its budget) needs only the smallest key.
-// The keys and values of the moved rows: by the same workgroup where few can move, or k_evict_move with workgroups for every
-// 64 moves.  Sources lie behind the budget and destinations below it, so no order is needed.
+// The keys and values of the moved rows: by the same workgroup where few can move, or k_evict_move with a wave for every 16 moves.  Sources lie behind the budget and destinations below it, so no order is needed.
 // =====================================================================================================
 __device__ __forceinline__ int lanes_before(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
@@ -1097,23 +1096,24 @@ __global__ __launch_bounds__(NT) void k_evict(const PagedEvictArgs a) {
   }
 }
 
-constexpr int EVICT_MOVES = 64;                        // moves of a workgroup: 16 a wave
+constexpr int EVICT_MOVES = 16;                        // moves of a workgroup, which is a wave
 
 // Many moves.  Bound by HBM: a value row's dims lie 64 bytes apart, each among the same dim of its step's other rows, so the lines of every
-// step that a row leaves or enters are read whole.  8191 -> 2048 rows in 16 heads of 128 dims (1640 moves each, 27 MB of rows in some
-// 60 MB of lines): 16.3 us.  (Whole steps through LDS, where the rows change places: 16.8 and 18.0 us, a wave for all dims and for a quarter.)
+// step that a row leaves or enters move.  8191 -> 2048 rows in 16 heads of 128 dims (1640 moves each, 27 MB of rows in 51 MB of lines):
+// 14.8 us; in workgroups of four waves 16.6 (416 of them on 256 compute units); whole steps through LDS, where the rows change places, 16.8
+// and 18.0 us (a wave for all dims, and for a quarter).
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_evict_move(const PagedEvictArgs a, int32_t *kv_len_out) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, unit = blockIdx.x;
+__global__ __launch_bounds__(WAVE) void k_evict_move(const PagedEvictArgs a, int32_t *kv_len_out) {
+  const int lane = threadIdx.x, unit = blockIdx.x;
   const int h = unit % a.c.n_kv, b = (unit / a.c.n_kv) % a.seqs.n_seq, layer = unit / (a.c.n_kv * a.seqs.n_seq);
-  if (!a.kv_len_out && h == 0 && layer == 0 && blockIdx.y == 0 && tid == 0) kv_len_out[b] = a.new_len[b];
+  if (!a.kv_len_out && h == 0 && layer == 0 && blockIdx.y == 0 && lane == 0) kv_len_out[b] = a.new_len[b];
   if (a.fused) return;
   const int n = a.n_moves[unit];
   const size_t base = (size_t)layer * a.c.layer_stride + (size_t)h * a.c.head_stride;
   const int2 *moves = a.moves + (size_t)unit * a.most;
   const size_t at = (size_t)unit * a.c.table_pages * a.c.page_rows;
-  for (int i0 = blockIdx.y * EVICT_MOVES + wave * 16; i0 < n; i0 += gridDim.y * EVICT_MOVES) {
-    if (lane < 16 && i0 + lane < n) {
+  for (int i0 = blockIdx.y * EVICT_MOVES; i0 < n; i0 += gridDim.y * EVICT_MOVES) {
+    if (lane < EVICT_MOVES && i0 + lane < n) {
       const int2 mv = moves[i0 + lane];
       a.weights_out[at + mv.x] = a.weights_in[at + mv.y];
       a.pos_out[at + mv.x] = a.pos_in[at + mv.y];
@@ -1154,9 +1154,9 @@ static hipError_t paged_evict_shape(hipStream_t st, PagedEvictArgs a, int n_laye
   else EVICT(1024, 0);
   #undef EVICT
   if (!a.fused)
-    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(units, std::min((a.most + EVICT_MOVES - 1) / EVICT_MOVES, 65535)), dim3(256), 0, st, a, len_out);
+    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(units, std::min((a.most + EVICT_MOVES - 1) / EVICT_MOVES, 65535)), dim3(WAVE), 0, st, a, len_out);
   else if (same_len)
-    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(a.seqs.n_seq * a.c.n_kv), dim3(256), 0, st, a, len_out);
+    hipLaunchKernelGGL((k_evict_move<T, DH>), dim3(a.seqs.n_seq * a.c.n_kv), dim3(WAVE), 0, st, a, len_out);
   return hipGetLastError();
 }
 

@@ -327,7 +327,8 @@ typedef struct amph_paged_kv {
 enum { AMPH_MAX_SEQ = 1024 };
 
 /* Bytes of scratch (16-byte aligned) for the calls below on a cache of this form.  n_layers = 0: amph_paged_attn without
- * weights; n_layers >= 1: amph_paged_attn with weights, and amph_paged_evict over so many layers. */
+ * weights; n_layers >= 1: amph_paged_attn with weights, and amph_paged_evict over so many layers.  A larger max_pages needs more.
+ * Nothing in it needs to start at zero, and nothing is left there for a later call; calls that overlap in time need one each. */
 amph_status amph_paged_bytes(amph_ctx *ctx, const amph_paged_kv *kv /* host */, int n_layers, size_t *bytes /* host */);
 
 /* Writes new rows into the pages of one layer.  For every sequence b and j < n_valid[b] (NULL: n_new; clamped to 0..n_new): the key,
@@ -348,7 +349,8 @@ amph_status amph_paged_append(amph_ctx *ctx, const amph_paged_kv *kv /* host */,
 /* Attention of one token of every sequence over its rows of one layer, rows = kv_len[b] + n_valid[b] (NULL: n_new; n_new = 0: kv_len[b]):
  *   out[b, i] = sum_r p_ir v_r,   p_i = softmax over the rows of q[b, i] . k_r / sqrt(head_dim),   r of key head i / (n_heads / n_kv_heads)
  *   weights_out[b, h, r] = weights_in[b, h, r] + sum of p_ir over the query heads i of key head h
- * A sequence without rows has out = 0.  Rows behind the last may hold anything.  No order of sums depends on timing.
+ * A sequence without rows, or with scores of -inf only, has out = 0.  Rows behind the last may hold anything.  Equal inputs give equal bits; where
+ * a long sequence's sums are cut depends on the lengths of all sequences and on max_pages, so its last bits may too.
  *   q   row b at b * ld_q elements, [n_heads, head_dim] T        out [n_seq, n_heads, head_dim] T, not q itself
  *   weights_in, weights_out [n_seq, n_kv_heads, table_pages * page_rows] float32: weights_out NULL: none are computed; weights_in NULL:
  *     zeros; they may be the same.  Places behind the last row are left as they are.

@@ -26,6 +26,13 @@ def workspace(ctx, kv, n_layers=0):
     return torch.full((ctx.amph_paged_workspace_bytes(kv, n_layers),), 0xff, dtype=torch.uint8, device=DEV)
 
 
+def off_by(x, floats):
+    """The same values in a tensor that begins `floats` elements behind an aligned address."""
+    buf = torch.empty(x.numel() + floats, dtype=x.dtype, device=DEV)
+    buf[floats:] = x.reshape(-1)
+    return buf[floats:].view(x.shape)
+
+
 # ---- attention ------------------------------------------------------------------------------------------------------------
 
 def attn_case(dtype, heads, n_kv, dim, lens, page=32, per=None, weights=None, layers=1, layer=0, ld_extra=0, scale=2.0, seed=0, max_pages=None):
@@ -414,7 +421,7 @@ def test_append_bad_lengths_and_pages():
 # ---- eviction -------------------------------------------------------------------------------------------------------------
 
 def evict_case(dtype, n_kv, dim, lens, budget, recent, page=32, layers=2, new=1, valid=None, weights="spread", positions="rows", in_place=False,
-               seed=0, per=None):
+               seed=0, per=None, shift=0):
     """lens: rows before the new ones."""
     news = [min(max(x, 0), new) for x in valid] if valid else [new] * len(lens)
     rows = [L + m for L, m in zip(lens, news)]
@@ -430,8 +437,8 @@ def evict_case(dtype, n_kv, dim, lens, budget, recent, page=32, layers=2, new=1,
         pos = (torch.argsort(torch.rand(shape, generator=g), -1) * 3 - 50).to(torch.int32)
     elif positions == "extreme":
         pos = torch.where(torch.rand(shape, generator=g) < 0.5, -2 ** 31, 2 ** 31 - 1).to(torch.int32)
-    w_in, p_in = w.to(DEV), pos.to(DEV)
-    w_out, p_out = (w_in, p_in) if in_place else (torch.full_like(w_in, -3.0), torch.full_like(p_in, -5))
+    w_in, p_in = off_by(w.to(DEV), shift), off_by(pos.to(DEV), shift)
+    w_out, p_out = (w_in, p_in) if in_place else (off_by(torch.full_like(w_in, -3.0), shift), off_by(torch.full_like(p_in, -5), shift))
     kv_len = i32(lens)
     len_out = kv_len if in_place else i32([-7] * n)
     before = [[pool.rows(ly, b) for b in range(n)] for ly in range(layers)]
@@ -499,6 +506,19 @@ def test_evict_new_rows_and_tables():
     evict_case("bf16", 2, 128, [90, 100, 3], 100, 5, new=20, valid=[20, 0, -1], per=9)
     evict_case("bf16", 2, 128, [90, 100, 3], 200, 5, new=20, valid=[25, 7, 1])
     evict_case("bf16", 2, 128, [90, 100, 3], 90, 0, new=0)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_weights_and_positions_anywhere(shift):
+    """Weights and positions begin on any element, as the header allows."""
+    evict_case("bf16", 3, 64, [300, 200, 20], 128, 7, shift=shift, page=64)
+    evict_case("f32", 3, 64, [3000, 128], 128, 7, shift=shift, page=64, layers=1, in_place=True)
+    pool, ctx = Pool("bf16", 2, 64, 32, [70, 200], 7), pr.make_ctx("bf16", 4, 64)
+    q, out = torch.randn(2, 4, 64, device=DEV).to(torch.bfloat16), torch.zeros(2, 4, 64, device=DEV, dtype=torch.bfloat16)
+    a, b = off_by(torch.rand(2, 2, pool.cap, device=DEV), shift), torch.zeros(2, 2, pool.cap, device=DEV)
+    ctx.amph_paged_attn(pool.kv, 0, q, 256, 0, None, i32([70, 200]), out, a, b, workspace(ctx, pool.kv, 1))
+    ctx.amph_paged_attn(pool.kv, 0, q, 256, 0, None, i32([70, 200]), out, a, a, workspace(ctx, pool.kv, 1))
+    assert torch.equal(a[0, :, :70], b[0, :, :70]) and torch.equal(a[1, :, :200], b[1, :, :200])
 
 
 def test_evict_bad_lengths_and_pages():
@@ -632,6 +652,54 @@ def test_decoding_with_a_budget_f32():
 def test_decoding_captured_and_replayed():
     """The same loop as one graph a step, its lengths, positions and idle sequences changing between replays; several workgroups a walk."""
     decode("bf16", 8, 2, 64, [700, 30], budget=600, recent=20, steps=8, layers=2, per=24, graph=True)
+
+
+@pytest.mark.parametrize("cfg,lens,budget", [(si.MINI, [77, 200, 5], 64), (si.TINY, [130, 100, 131], 100)])
+def test_the_step_s_caches_appended_to_evicted_and_verified(cfg, lens, budget):
+    """The caches of amph_target_forward, three layers of them: rows appended where they lie, every head held to a budget, and the tree attention
+    over what is left, with a tree whose rows come behind it."""
+    d_h, n_h, bsz, max_kv, layers, n_new = cfg.head_dim, cfg.n_heads, 3, 256, 3, 3
+    ctx = B.Context(d_model=n_h * d_h, n_heads=n_h, head_dim=d_h, d_ffn=64, vocab=64, K=4, topk=4, max_tree=8, max_kv=max_kv, batch=bsz,
+                    dtype=D.dtype_code(cfg.dtype), device=DEV)
+    tdt, tree = D.torch_dtype(cfg.dtype), B.Tree(si.tree_paths(8, (4, 2, 2, 2)), 4)
+    g = torch.Generator().manual_seed(11)
+    k, v = (torch.randn(layers, bsz, n_h, max_kv, d_h, generator=g).to(tdt) for _ in range(2))
+    kc, vc = lr.keys_to_tiled(k).to(DEV), lr.values_to_tiled(v).to(DEV)
+    kv, table = D.paged_caches(kc, vc, 64)
+    w = torch.rand(layers, bsz, n_h, max_kv, generator=g)
+    pos = torch.arange(max_kv, dtype=torch.int32).expand(layers, bsz, n_h, max_kv).contiguous()
+    w_d, p_d, n, out_n = w.to(DEV), pos.to(DEV), i32(lens), i32([0] * bsz)
+    new = torch.randn(layers, bsz, n_new, 2 * n_h * d_h, generator=g).to(tdt)
+    d = new.to(DEV)
+    for ly in range(layers):
+        x = d[ly]
+        ctx.amph_paged_append(kv, ly, n_new, None, n, None, None, 0, x, 2 * n_h * d_h, x[..., n_h * d_h:], 2 * n_h * d_h, None, w_d[ly], p_d[ly])
+    k, v = lr.tiled_to_keys(kc.cpu()), lr.tiled_to_values(vc.cpu())        # (the appended rows: checked here against the new ones)
+    for b, L in enumerate(lens):
+        rows = new[:, b, :, :n_h * d_h].view(layers, n_new, n_h, d_h)
+        ref = pr.turn(rows, (L + torch.arange(n_new))[:, None].expand(n_new, n_h), 10000.0)
+        assert bool(((k[:, b, :, L:L + n_new].transpose(1, 2).to(F64) - ref).abs() <= pr.turn_bounds(cfg.dtype, rows, ref)).all())
+        assert torch.equal(v[:, b, :, L:L + n_new].transpose(1, 2), new[:, b, :, n_h * d_h:].view(layers, n_new, n_h, d_h))
+        w[:, b, :, L:L + n_new] = 0.0
+    ctx.amph_paged_evict(kv, layers, budget, 10, n_new, None, n, out_n, w_d, w_d, p_d, p_d, workspace(ctx, kv, layers))
+    q, out = torch.randn(bsz, 8, n_h, d_h, generator=g).to(tdt), torch.zeros(bsz, 8, n_h, d_h, dtype=tdt, device=DEV)
+    assert out_n.tolist() == [min(L + n_new, budget) for L in lens]
+    mask = torch.from_numpy(tree.mask_bool())
+    for ly in range(layers):
+        ctx.amph_verify_attn(tree, q.to(DEV), kc[ly], vc[ly], out_n, out)
+        k_now, v_now = lr.tiled_to_keys(kc[ly].cpu()), lr.tiled_to_values(vc[ly].cpu())
+        for b, L in enumerate(lens):
+            for h in range(n_h):
+                at = pr.evict_rows(w[ly, b, h].tolist(), pos[ly, b, h].tolist(), L + n_new, budget, 10)
+                m = len(at)
+                keys = torch.cat([k[ly, b, h, torch.tensor(at)], k_now[b, h, m:m + 8]])        # (the tree's rows: whatever lies there)
+                vals = torch.cat([v[ly, b, h, torch.tensor(at)], v_now[b, h, m:m + 8]])
+                for node in range(8):
+                    see = torch.cat([torch.ones(m, dtype=torch.bool), mask[node]])
+                    ref, _, mag, reach = pr.attn(q[b, node, h:h + 1], keys[None, see], vals[None, see])
+                    most = pr.attn_bounds(cfg.dtype, ref, mag, reach, m + 8, d_h) + (mag * 2.0 ** -8 if cfg.dtype == "bf16" else 0.0)
+                    assert bool(((out[b, node, h:h + 1].cpu().to(F64) - ref).abs() <= most).all()), (ly, b, h, node)
+    assert ctx.device_status() == 0
 
 
 def test_two_streams_with_workspaces_of_their_own():

@@ -321,7 +321,8 @@ typedef struct amph_paged_kv {
   int32_t n_pages;              /* entries outside [0, n_pages) are refused (AMPH_DEV_BAD_PAGE)                     */
   int32_t table_pages;          /* entries of a row of the table; table_pages * page_rows <= 2^24                   */
   int32_t max_pages;            /* 1..table_pages: no sequence has rows beyond these pages in the calls it is given to.
-                                   A tight bound saves launches and workspace where sequences are short              */
+                                   A tight bound saves launches and workspace where sequences are short.
+                                   n_seq * cfg.n_heads * max_pages * page_rows <= 2^33; n_layers * n_seq * n_kv_heads <= 2^21 */
   int64_t page_stride, head_stride, layer_stride;   /* elements; multiples of 16 bytes                              */
 } amph_paged_kv;
 enum { AMPH_MAX_SEQ = 1024 };

@@ -786,8 +786,9 @@ const char *paged_kv_fault(const amph_config &c, const amph_paged_kv *kv, int n_
   constexpr int64_t far = (int64_t)1 << 46;                // elements: offsets in bytes stay below 2^48 each
   if (kv->page_stride > far / kv->n_pages || kv->head_stride > far / kv->n_kv_heads || kv->layer_stride > far / std::max(n_layers, 1))
     return "strides too large";
-  if ((int64_t)std::max(n_layers, 1) * kv->n_seq * kv->n_kv_heads > (1 << 30)) return "too many layers";
-  if ((int64_t)kv->n_seq * c.n_heads * kv->max_pages * kv->page_rows > (int64_t)1 << 40) return "too many rows in all";
+  // a launch has fewer than 2^32 threads: 1024 for every layer, sequence and key head, or 256 for every 1024 rows of a sequence and key head
+  if ((int64_t)std::max(n_layers, 1) * kv->n_seq * kv->n_kv_heads > (1 << 21)) return "more than 2^21 layers, sequences and key heads";
+  if ((int64_t)kv->n_seq * c.n_heads * kv->max_pages * kv->page_rows > (int64_t)1 << 33) return "more than 2^33 rows over all sequences and heads";
   return nullptr;
 }
 }  // namespace amph

@@ -534,10 +534,9 @@ static hipError_t paged_attn_shape(hipStream_t st, PagedAttnArgs a) {
   else
     hipLaunchKernelGGL((k_paged_attn<T, DH, NQB, false>), dim3(PAGED_WGS), dim3(256), 0, st, a);
   const int row_wgs = weights ? (a.seqs.cap + PAGED_WROWS - 1) / PAGED_WROWS : 0;
-  const long long grid = (alone ? 0ll : (long long)a.seqs.n_seq * a.n_heads) + (long long)a.seqs.n_seq * a.c.n_kv * row_wgs;
-  if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+  const unsigned grid = (alone ? 0 : a.seqs.n_seq * a.n_heads) + a.seqs.n_seq * a.c.n_kv * row_wgs;
   if (grid)
-    hipLaunchKernelGGL((k_paged_fold<T, DH, NQB>), dim3((unsigned)grid), dim3(256), 0, st, a, alone, std::max(row_wgs, 1));
+    hipLaunchKernelGGL((k_paged_fold<T, DH, NQB>), dim3(grid), dim3(256), 0, st, a, alone, std::max(row_wgs, 1));
   return hipGetLastError();
 }
 

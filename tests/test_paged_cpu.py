@@ -134,7 +134,7 @@ def fault(n_layers=1, cfg=None, null=False, **kw):
 
 def test_a_sound_cache_is_taken():
     assert fault() is None and fault(n_layers=0) is None and fault(max_pages=1, n_kv_heads=1, page_rows=32) is None
-    assert fault(n_seq=1024, table_pages=2 ** 18, max_pages=2 ** 18) is None and fault(layer_stride=0) is None
+    assert fault(n_seq=128, table_pages=2 ** 18, max_pages=2 ** 18) is None and fault(n_layers=2 ** 20, n_seq=1, layer_stride=64) is None and fault(layer_stride=0) is None
     assert fault(page_stride=2 ** 42, layer_stride=2 ** 45, n_layers=2) is None
     assert fault(cfg=base_cfg(dtype=B.AMPH_BF16)) is None
 
@@ -146,6 +146,7 @@ def test_a_sound_cache_is_taken():
     (dict(layer_stride=2), False), (dict(n_layers=-1), False),
     (dict(n_seq=1025), True), (dict(n_kv_heads=3), True), (dict(page_rows=48), True), (dict(page_rows=16), True), (dict(max_pages=5), True),
     (dict(table_pages=2 ** 18 + 1), True), (dict(page_stride=2 ** 43), True), (dict(head_stride=2 ** 46), True), (dict(layer_stride=2 ** 45, n_layers=3), True), (dict(n_layers=2 ** 30), True),
+    (dict(n_layers=2 ** 20 + 1, n_seq=1, layer_stride=64), True), (dict(n_seq=129, table_pages=2 ** 18, max_pages=2 ** 18), True),
     (dict(n_seq=1024, table_pages=2 ** 18, max_pages=2 ** 18, cfg=base_cfg(n_heads=128, d_model=8192)), True),
 ])
 def test_an_unsound_cache_is_refused(kw, shape):

@@ -552,8 +552,8 @@ template hipError_t launch_paged_attn<bf16_t>(hipStream_t, const PagedAttnArgs &
 // =====================================================================================================
 // amph_paged_append
 // A workgroup has one key step's rows of one sequence (those of them that are new) for some of the heads: first the rows' cosines
-// and sines into LDS, then a wave takes head after head.  A whole step of values is turned round in registers, so that its
-// lines are written whole; of a part of one every element is written on its own.
+// and sines into LDS, then a wave takes head after head.  A step's values are turned round in registers, so that runs of rows are
+// written at once; a few rows, as of a decoding step, and the ends among a lane's rows element by element.
 // =====================================================================================================
 // Sine and cosine of an angle in turns: the nearest quarter turn is taken off in 64 bits, what is left, up to half a quarter, goes through
 // the Taylor polynomials (their next terms are 2e-9 and 2.5e-8 there), and the quarters swap and negate the two.
@@ -645,24 +645,51 @@ __global__ __launch_bounds__(256) void k_paged_append(const PagedAppendArgs a, c
     } else {
       const T *src = (const T *)a.v + new0 * a.ld_v + (size_t)h * DH;
       T *dst = (T *)a.c.v + page + (size_t)h * a.c.head_stride;
-      if (live == KSTEP) {
-        constexpr int UN = DH / 16, LPV = DH / PER;    // a lane has UN adjacent rows of PER adjacent dims
+      // all rows are asked for before the first is stored (past the last one: that again)
+      auto few = [&](auto tag) {
+        constexpr int N = decltype(tag)::value;
+        T x[N][DH / WAVE];
+        #pragma unroll
+        for (int r = 0; r < N; ++r)
+          #pragma unroll
+          for (int c = 0; c < DH / WAVE; ++c) x[r][c] = src[(size_t)min(r, live - 1) * a.ld_v + c * WAVE + lane];
+        #pragma unroll
+        for (int r = 0; r < N; ++r) {
+          if (r >= live) break;
+          #pragma unroll
+          for (int c = 0; c < DH / WAVE; ++c) dst[v_tiled_index<T>(k0 + r, c * WAVE + lane, DH)] = x[r][c];
+        }
+      };
+      if (live == 1) {
+        few(Rows<1>{});
+      } else if (live <= 4) {
+        few(Rows<4>{});
+      } else {
+        constexpr int UN = DH / 16, LPV = DH / PER;    // a lane has UN adjacent rows of the step, PER adjacent dims of each
         typedef T run __attribute__((ext_vector_type(UN)));
-        const int li = lane % LPV, grp = lane / LPV;
+        const int li = lane % LPV, first = (lane / LPV) * UN;
         frag x[UN];
         #pragma unroll
-        for (int j = 0; j < UN; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const frag *>(src + (size_t)(grp * UN + j) * a.ld_v + li * PER));
-        #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-          run y;
-          #pragma unroll
-          for (int j = 0; j < UN; ++j) y[j] = x[j][e];
-          *reinterpret_cast<run *>(dst + v_tiled_index<T>(grp * UN, li * PER + e, DH)) = y;
+        for (int j = 0; j < UN; ++j) {
+          const int r = min(max(first + j - k0, 0), live - 1);
+          x[j] = __builtin_nontemporal_load(reinterpret_cast<const frag *>(src + (size_t)r * a.ld_v + li * PER));
         }
-      } else {
-        for (int r = 0; r < live; ++r)
+        if (first >= k0 && first + UN <= k0 + live) {
           #pragma unroll
-          for (int c = lane; c < DH; c += WAVE) dst[v_tiled_index<T>(k0 + r, c, DH)] = src[(size_t)r * a.ld_v + c];
+          for (int e = 0; e < PER; ++e) {
+            run y;
+            #pragma unroll
+            for (int j = 0; j < UN; ++j) y[j] = x[j][e];
+            *reinterpret_cast<run *>(dst + v_tiled_index<T>(first, li * PER + e, DH)) = y;
+          }
+        } else {                                       // an end of the new rows lies among the lane's: one by one
+          #pragma unroll
+          for (int j = 0; j < UN; ++j) {
+            if (first + j < k0 || first + j >= k0 + live) continue;
+            #pragma unroll
+            for (int e = 0; e < PER; ++e) dst[v_tiled_index<T>(first + j, li * PER + e, DH)] = x[j][e];
+          }
+        }
       }
     }
   }
@@ -672,10 +699,12 @@ template <typename T>
 hipError_t launch_paged_append(hipStream_t st, const PagedAppendArgs &a, const PagedRope &rope, int d_h) {
   constexpr int KSTEP = 4 * Elem<T>::PER;
   const int steps = (a.seqs.n_new + KSTEP - 2) / KSTEP + 1, units = (a.q ? a.n_heads : 0) + 2 * a.c.n_kv;
-  // Heads are spread over workgroups until there are four for every compute unit, as many heads for every wave (four prompts of 256 to
-  // 1024 rows, 32 heads of 128 dims and as many key heads, us: one to a wave 30.6, two 28.9 and 34.0, three 27.5, six 34.3).
-  const long long have = (long long)steps * a.seqs.n_seq;
-  const int m = (int)std::max<long long>(1, std::min<long long>(units, units * have / 4096)), z = (units + 4 * m - 1) / (4 * m);
+  // Heads are spread over workgroups, as many for every wave.  3072 waves are resident at once; beyond, one head each would start anew for the rest, and
+  // with unequal prompts part of the grid is idle.  Measured (us, heads a wave: 128 dims, bf16): four prompts of 256 to 1024 rows, 32 heads and as many key
+  // heads, 1: 31.2, 2: 34.6, 3: 27.5, 4: 31.1, 6: 34.5; two of 1340 rows, 32 and 8 heads, 1: 22.1, 2: 18.5, 3: 19.9; one of 512 rows, 32 and
+  // 32 heads, 1: 10.0, 2: 11.6.
+  const long long all = (long long)steps * a.seqs.n_seq * units;
+  const int m = (int)std::min<long long>(units, std::max<long long>(all / 4096, all > 3072 ? 2 : 1)), z = (units + 4 * m - 1) / (4 * m);
   const dim3 grid(steps, a.seqs.n_seq, z);
   if (d_h == 128) hipLaunchKernelGGL((k_paged_append<T, 128>), grid, dim3(256), 0, st, a, rope);
   else hipLaunchKernelGGL((k_paged_append<T, 64>), grid, dim3(256), 0, st, a, rope);

@@ -729,12 +729,12 @@ template <typename T>
 hipError_t launch_paged_append(hipStream_t st, const PagedAppendArgs &a, const PagedRope &rope, int d_h) {
   constexpr int KSTEP = 4 * Elem<T>::PER;
   const int steps = (a.seqs.n_new + KSTEP - 2) / KSTEP + 1, units = (a.q ? a.n_heads : 0) + 2 * a.c.n_kv;
-  // Heads are spread over workgroups, as many for every wave.  3072 waves are resident at once; beyond, one head each would start anew for the rest, and
+  // Heads are spread over workgroups, as many for every wave.  Twelve waves are resident on each of 256 compute units; beyond, one head each would start anew for the rest, and
   // with unequal prompts part of the grid is idle.  Measured (us, heads a wave: 128 dims, bf16): four prompts of 256 to 1024 rows, 32 heads and as many key
   // heads, 1: 31.2, 2: 34.6, 3: 27.5, 4: 31.1, 6: 34.5; two of 1340 rows, 32 and 8 heads, 1: 22.1, 2: 18.5, 3: 19.9; one of 512 rows, 32 and
   // 32 heads, 1: 10.0, 2: 11.6.
   const long long all = (long long)steps * a.seqs.n_seq * units;
-  const int m = (int)std::min<long long>(units, std::max<long long>(all / 4096, all > 3072 ? 2 : 1)), z = (units + 4 * m - 1) / (4 * m);
+  const int m = (int)std::min<long long>(units, std::max<long long>(all / 4096, all > 12 * 256 ? 2 : 1)), z = (units + 4 * m - 1) / (4 * m);
   const dim3 grid(steps, a.seqs.n_seq, z);
   if (d_h == 128) hipLaunchKernelGGL((k_paged_append<T, 128>), grid, dim3(256), 0, st, a, rope);
   else hipLaunchKernelGGL((k_paged_append<T, 64>), grid, dim3(256), 0, st, a, rope);
